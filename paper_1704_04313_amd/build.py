@@ -7,8 +7,10 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcbinfer_hip.so")
-SOURCES = ["cbinfer.hip", "kernels_maps.hip", "kernels_gemm.hip"]
-HEADERS = ["kernels.h", os.path.join("..", "..", "include", "cbinfer.h")]
+SOURCES = ["cbinfer.hip", "kernels_maps.hip", "kernels_gemm.hip", "tokens.hip", "kernels_scores.hip", "kernels_attention.hip",
+           "kernels_product.hip", "kernels_norm.hip"]
+HEADERS = ["kernels.h", "tokens.h", os.path.join("..", "..", "include", "cbinfer.h"),
+           os.path.join("..", "..", "include", "cbinfer_tokens.h")]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

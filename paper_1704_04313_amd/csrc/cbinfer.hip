@@ -4,6 +4,7 @@
 // kernels of a frame on the caller's stream without ever waiting for the device.
 #include "../../include/cbinfer.h"
 #include "kernels.h"
+#include "tokens.h"
 
 #include <algorithm>
 #include <cmath>
@@ -285,6 +286,15 @@ struct EventPair {
 };
 
 } // namespace
+
+int cbk::set_error(int code, const char *message) noexcept
+{
+    try {
+        return fail(code, "%s", message);
+    } catch (...) { // no memory for the message
+        return code;
+    }
+}
 
 struct cbinfer_state {
     Plan plan;

@@ -1,0 +1,148 @@
+"""Products with 4-bit weights against 64 bits: every code, sizes that end inside a group, a block and a tile, strides,
+values that are not finite."""
+import pytest
+import torch
+
+import paper_1704_04313_amd as cb
+from token_util import U, VALUES, assert_within, weights64
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.float32, torch.bfloat16]
+
+
+def _layer(n, k, group, seed, bias=True):
+    g = torch.Generator().manual_seed(seed)
+    codes = torch.randint(0, 16, (n, k), generator=g, dtype=torch.uint8)
+    scales = (0.02 + torch.rand(n, -(-k // group), generator=g)).to(torch.bfloat16)
+    b = torch.randn(n, generator=g) if bias else None
+    return codes, scales, b, cb.QuantisedLinear(codes.cuda(), scales.cuda(), None if b is None else b.cuda(), group=group)
+
+
+def _check(y, x, codes, scales, bias, group, what):
+    """A sum of k products in float32, in any order: 4 sqrt(k) roundings of the sum over magnitudes at the very most, some for
+    scales and bias."""
+    w, x64 = weights64(codes, scales, group), x.detach().cpu().double()
+    want, most = x64 @ w.t(), x64.abs() @ w.abs().t()
+    if bias is not None:
+        want, most = want + bias.double(), most + bias.double().abs()
+    assert_within(y, want, (32 + 4 * w.shape[1] ** 0.5) * U * most, what)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k,group", [(1, 1, 1, 32), (1, 16, 128, 32), (1, 17, 129, 64), (2, 100, 300, 128), (3, 64, 1000, 32),
+                                         (5, 33, 31, 64), (7, 256, 4096, 64), (16, 48, 640, 128), (17, 80, 100, 32), (33, 500, 256, 64),
+                                         (64, 96, 2000, 128), (65, 40, 160, 32), (100, 16, 5000, 64), (130, 200, 136, 128), (1, 2999, 512, 32),
+                                         (64, 256, 9600, 128), (12, 20, 20000, 64)])
+def test_sizes(m, n, k, group, dtype):
+    codes, scales, bias, layer = _layer(n, k, group, m + n + k, bias=n % 2 == 0)
+    x = torch.randn(m, k, generator=torch.Generator().manual_seed(1)).to(dtype).cuda()
+    _check(layer(x), x, codes, scales, bias, group, "%dx%dx%d" % (m, n, k))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_every_code_in_every_place(group, dtype):
+    """One token at a time picks one column: the weights themselves come back, exactly."""
+    n, k = 40, 300
+    codes, scales, _, layer = _layer(n, k, group, 3, bias=False)
+    y = layer(torch.eye(k, dtype=dtype, device="cuda"))
+    w = weights64(codes, scales, group)
+    assert torch.equal(y.cpu().double(), w.t().to(dtype).double())
+
+
+@pytest.mark.parametrize("m", [1, 4, 20, 64])
+def test_integers_exactly(m):
+    n, k, group = 200, 2500, 64
+    g = torch.Generator().manual_seed(8)
+    codes = torch.randint(0, 16, (n, k), generator=g, dtype=torch.uint8)
+    scales = torch.tensor([2.0, 4.0, 8.0])[torch.randint(0, 3, (n, -(-k // group)), generator=g)].to(torch.bfloat16)
+    x = torch.randint(-6, 7, (m, k), generator=g).float()
+    y = cb.QuantisedLinear(codes.cuda(), scales.cuda(), group=group)(x.cuda())
+    assert torch.equal(y.cpu().double(), x.double() @ weights64(codes, scales, group).t())
+
+
+def test_float32_values_keep_24_bits():
+    """x of 24 bits times powers of two: nothing is lost when x is taken apart."""
+    k = 64
+    codes = torch.full((16, k), 2, dtype=torch.uint8)
+    scales = torch.ones(16, 1, dtype=torch.bfloat16)
+    layer = cb.QuantisedLinear(codes.cuda(), scales.cuda(), group=64)
+    x = torch.zeros(6, k)
+    x[:, 7] = torch.tensor([1 + 2.0 ** -23, 3.4028234e38, -1.1754944e-27, 16777215.0, 0.1, -1e30])
+    assert torch.equal(layer(x.cuda()).cpu(), x[:, 7:8].expand(6, 16))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_not_finite(dtype):
+    codes, scales, _, layer = _layer(32, 200, 64, 5, bias=False)
+    x = torch.randn(5, 200, generator=torch.Generator().manual_seed(2)).to(dtype)
+    x[0, 3], x[1, 150], x[2, 199], x[3, 0] = float("inf"), float("nan"), float("-inf"), float("inf")
+    x[3, 1] = float("-inf")
+    want = x.double() @ weights64(codes, scales, 64).t()
+    got = layer(x.cuda()).cpu().double()
+    assert torch.equal(got.isnan(), want.isnan())
+    assert torch.equal(got[got.isinf()], want[want.isinf()])
+    assert torch.equal(got.isinf(), want.isinf()) and got[4].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_strides_and_shapes(dtype):
+    codes, scales, bias, layer = _layer(70, 260, 64, 6)
+    wide = torch.randn(3, 5, 700, generator=torch.Generator().manual_seed(3)).to(dtype).cuda()
+    for at in (0, 1, 4, 8):
+        x = wide[..., at:at + 260]
+        _check(layer(x).view(15, 70), x.reshape(15, 260), codes, scales, bias, 64, "part from %d" % at)
+    x = wide[0, 0, 3:263]
+    assert layer(x).shape == (70,)
+    _check(layer(x)[None], x[None], codes, scales, bias, 64, "vector")
+    out = torch.empty(15, 70, dtype=dtype, device="cuda")
+    assert layer(wide.view(15, 700)[:, :260], out=out) is out
+    _check(out, wide.view(15, 700)[:, :260], codes, scales, bias, 64, "out")
+    assert layer(wide[:0, :, :260]).shape == (0, 5, 70)
+
+
+def test_same_bits_alone_and_among_others():
+    """A token's result does not depend on the tokens beside it in its tile, nor on the stream."""
+    _, _, _, layer = _layer(300, 1500, 32, 9)
+    x = torch.randn(16, 1500, generator=torch.Generator().manual_seed(5)).cuda()
+    y = layer(x)
+    assert torch.equal(y, layer(x))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        z = layer(x)
+    side.synchronize()
+    assert torch.equal(y, z)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_quantising(group, dtype):
+    g = torch.Generator().manual_seed(10)
+    w = torch.randn(37, 333, generator=g).to(dtype)
+    w[3] = 0.0
+    w[4, :40] *= 1e-3
+    codes, scales = (t.cpu() for t in cb.quantise_weights(w.cuda(), group))
+    w64 = w.double()
+    for n in range(37):
+        for a in range(0, 333, group):
+            part, s = w64[n, a:a + group], float(scales[n, a // group])
+            assert s == float((part.abs().max().float() / 6).to(torch.bfloat16))
+            c = codes[n, a:a + group].long()
+            if s == 0:
+                assert not c.any()
+                continue
+            near = ((part / s)[:, None] - VALUES[None, :]).abs()
+            # the quotient is rounded to float32 before it is compared: at most that far from the nearest
+            assert bool((near.gather(1, c[:, None])[:, 0] <= near.min(1).values + 8 * U).all())
+    layer = cb.QuantisedLinear.from_weights(w.cuda(), group=group)
+    x = torch.randn(3, 333, generator=g).to(dtype).cuda()
+    _check(layer(x), x, codes, scales, None, group, "from weights")
+
+
+def test_ties_take_the_even_code():
+    w = torch.zeros(1, 32)
+    w[0, :16] = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, -0.25, -0.75, -1.25, -1.75, -2.5, -3.5, -5.0, -6.0])
+    codes, scales = cb.quantise_weights(w.cuda(), 32)
+    assert float(scales) == 1.0
+    assert codes[0, :16].tolist() == [0, 2, 2, 4, 4, 6, 6, 7, 0, 10, 10, 12, 12, 14, 14, 15]

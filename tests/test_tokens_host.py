@@ -1,0 +1,156 @@
+"""Token operators without a GPU: the library exports what the header declares, refuses bad arguments with a message
+before it touches the device, and so do the Python entry points."""
+import ctypes as C
+import os
+import re
+
+import pytest
+import torch
+
+import paper_1704_04313_amd as cb
+from paper_1704_04313_amd import tokens
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def test_library_exports_every_declared_function():
+    src = open(os.path.join(ROOT, "include", "cbinfer_tokens.h")).read()
+    src = re.sub(r"/\*.*?\*/", "", src, flags=re.S)
+    names = sorted(set(re.findall(r"\b(cbinfer_[a-z_]+)\s*\(", src)))
+    assert names == sorted(tokens.EXPORTS)
+    lib = cb.load_library()
+    for n in names:
+        assert hasattr(lib, n), n
+
+
+@pytest.mark.parametrize("name", ["log_probs", "linear_attention", "quantised_product", "gated_norm"])
+def test_structures_are_as_long_as_the_header_says(name, tmp_path):
+    """The C compiler's size and the offset of every field against the binding's."""
+    args = getattr(tokens, name + "_args")
+    lines = ['printf("%zu", sizeof(cbinfer_' + name + '_args));']
+    lines += ['printf(" %%zu", offsetof(cbinfer_%s_args, %s));' % (name, f[0]) for f in args._fields_]
+    src = tmp_path / "s.c"
+    src.write_text('#include <stdio.h>\n#include "%s/include/cbinfer_tokens.h"\nint main(void){%s return 0;}' % (ROOT, "".join(lines)))
+    import subprocess
+    subprocess.run(["gcc", "-std=c99", "-o", str(tmp_path / "s"), str(src)], check=True)
+    got = [int(v) for v in subprocess.run([str(tmp_path / "s")], check=True, capture_output=True, text=True).stdout.split()]
+    assert got == [C.sizeof(args)] + [getattr(args, f[0]).offset for f in args._fields_]
+
+
+def _bad(call, args, changes, message):
+    lib = tokens._library()
+    a = args.__class__.from_buffer_copy(args)
+    for name, value in changes.items():
+        setattr(a, name, value)
+    assert getattr(lib, call)(a, None) < 0
+    assert message in lib.cbinfer_last_error().decode()
+
+
+@pytest.mark.parametrize("changes,message", [
+    (dict(dtype=2), "dtype"), (dict(outer=-1), "outer"), (dict(outer=1 << 20, inner=1 << 20), "2^31"), (dict(classes=0), "classes"),
+    (dict(classes=1 << 31), "classes"), (dict(top=-1), "top"), (dict(top=65), "top"), (dict(top=11), "top"),
+    (dict(labels=64, label=64, label_bytes=2), "label_bytes"), (dict(label=64), "without labels"), (dict(scores=None), "scores"),
+    (dict(scores=66), "scores"), (dict(top=2), "top_values"), (dict(entropy=None), "no output"), (dict(entropy=66), "aligned"),
+])
+def test_log_probs_refuses(changes, message):
+    a = tokens.log_probs_args(dtype=0, outer=3, classes=10, inner=1, outer_stride=10, class_stride=1, inner_stride=1, scores=64, entropy=64)
+    _bad("cbinfer_log_probs", a, changes, message)
+
+
+@pytest.mark.parametrize("changes,message", [
+    (dict(dtype=-1), "dtype"), (dict(streams=-1), ">= 0"), (dict(tokens=-1), ">= 0"), (dict(kv_heads=0), "multiple"), (dict(kv_heads=3), "multiple"),
+    (dict(key_size=0), "1 .. 256"), (dict(value_size=257), "1 .. 256"), (dict(scale=float("inf")), "scale"), (dict(q=None), "q, k, v"),
+    (dict(o=65), "q, k, v"), (dict(state=None), "state"), (dict(decay=66), "state and decay"), (dict(lengths=66), "lengths"),
+    (dict(streams=1 << 20, heads=64), "2^24"),
+])
+def test_linear_attention_refuses(changes, message):
+    a = tokens.linear_attention_args(dtype=0, streams=1, tokens=1, heads=4, kv_heads=2, key_size=8, value_size=8, scale=1.0, q=64, k=64, v=64,
+                                     o=64, state=64, decay=64)
+    _bad("cbinfer_linear_attention", a, changes, message)
+
+
+@pytest.mark.parametrize("changes,message", [
+    (dict(dtype=5), "dtype"), (dict(group=16), "group"), (dict(group=0), "group"), (dict(rows=0), "rows and cols"), (dict(cols=-1), "rows and cols"),
+    (dict(tokens=-1), "tokens"), (dict(tokens=1 << 21), "tokens"), (dict(x=None), "x and y"), (dict(y=66), "x and y"), (dict(packed=128), "packed"),
+    (dict(packed=None), "packed"), (dict(bias=66), "bias"),
+])
+def test_quantised_product_refuses(changes, message):
+    a = tokens.quantised_product_args(dtype=0, group=64, tokens=1, rows=8, cols=8, x_stride=8, y_stride=8, x=256, packed=256, y=256)
+    _bad("cbinfer_quantised_product", a, changes, message)
+
+
+@pytest.mark.parametrize("changes,message", [
+    (dict(dtype=7), "dtype"), (dict(sum_dtype=1), "sum_dtype"), (dict(rows=-1), "rows"), (dict(size=0), "size"), (dict(size=16385), "16384"),
+    (dict(group=3), "group"), (dict(group=-2), "group"), (dict(gate_kind=3), "gate_kind"), (dict(gate_kind=1), "go together"), (dict(gate=64), "go together"),
+    (dict(eps=-1.0), "eps"), (dict(eps=float("nan")), "eps"), (dict(scale=float("nan")), "scale"), (dict(x=None), "x must"), (dict(h=None), "no output"),
+    (dict(y=64), "go together"), (dict(next_weight=64), "go together"), (dict(residual=66), "aligned"),
+])
+def test_gated_norm_refuses(changes, message):
+    a = tokens.gated_norm_args(dtype=0, rows=1, size=8, x_stride=8, h_stride=8, scale=1.0, eps=1e-6, x=64, h=64)
+    _bad("cbinfer_gated_norm", a, changes, message)
+
+
+def test_null_arguments():
+    lib = tokens._library()
+    for name in ("log_probs", "linear_attention", "quantised_product", "gated_norm"):
+        assert getattr(lib, "cbinfer_" + name)(None, None) == -1
+        assert "NULL" in lib.cbinfer_last_error().decode()
+    for name in ("log_probs", "linear_attention", "quantised_product"):
+        assert getattr(lib, "cbinfer_%s_workspace_bytes" % name)(None) == 0
+    assert lib.cbinfer_pack_weights(None, None, 8, 8, 64, None, None) == -1
+    assert lib.cbinfer_quantise_weights(None, 0, 8, 8, 8, 64, None, None, None) == -1
+
+
+def test_packed_weights_take_half_a_byte_and_their_scales():
+    lib = tokens._library()
+    assert lib.cbinfer_packed_weights_bytes(16, 128, 64) == 16 * 64 + 16 * 2 * 2
+    assert lib.cbinfer_packed_weights_bytes(17, 129, 32) == 4 * (1024 + 16 * 4 * 2)
+    for rows, cols, group in ((0, 8, 64), (8, 0, 64), (8, 8, 16), (-5, 8, 64), (1 << 29, 8, 64)):
+        assert lib.cbinfer_packed_weights_bytes(rows, cols, group) == 0
+
+
+def test_tensors_on_the_cpu_are_refused():
+    x = torch.zeros(4, 8)
+    for call in (lambda: cb.log_probs(x), lambda: cb.gated_norm(x), lambda: cb.quantise_weights(x),
+                 lambda: cb.QuantisedLinear(torch.zeros(4, 8, dtype=torch.uint8), torch.zeros(4, 1, dtype=torch.bfloat16))):
+        with pytest.raises(cb.CBInferError):
+            call()
+    if not torch.cuda.is_available():
+        with pytest.raises(cb.CBInferError, match="no GPU"):
+            cb.LinearAttention([0.9], 8, 8)
+
+
+@pytest.mark.gpu
+def test_python_entry_points_refuse():
+    x = torch.zeros(4, 8, device="cuda")
+    b = torch.zeros(4, 8, 3, 5, device="cuda")
+    w8, i = torch.ones(8, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+    codes, scales = torch.zeros(6, 8, dtype=torch.uint8, device="cuda"), torch.zeros(6, 1, dtype=torch.bfloat16, device="cuda")
+    layer = cb.QuantisedLinear(codes, scales)
+    att = cb.LinearAttention([0.9, 0.8], 8, 8, n_streams=2, kv_heads=1)
+    q, k = torch.zeros(2, 3, 2, 8, device="cuda"), torch.zeros(2, 3, 1, 8, device="cuda")
+    for call, message in (
+            (lambda: cb.log_probs(x.half()), "float32 or bfloat16"), (lambda: cb.log_probs(x, dim=2), "no axis"), (lambda: cb.log_probs(x, top=9), "top"),
+            (lambda: cb.log_probs(x, i[:3]), "shape"), (lambda: cb.log_probs(x, i.short()), "int32 or int64"), (lambda: cb.log_probs(x, i.cpu()), "expected"),
+            (lambda: cb.log_probs(b[..., ::2, :4].contiguous()[..., :3]), "behind"),
+            (lambda: cb.gated_norm(x, w8[:7]), "8 values"), (lambda: cb.gated_norm(x, w8, group=3), "divide"), (lambda: cb.gated_norm(x, group=4), "group without"),
+            (lambda: cb.gated_norm(x, gate=x), "go together"), (lambda: cb.gated_norm(x, gate=x, activation="tanh"), "go together"),
+            (lambda: cb.gated_norm(x, gate=x.bfloat16(), activation="silu"), "type of x"), (lambda: cb.gated_norm(x, residual=x[:3]), "shape of x"),
+            (lambda: cb.gated_norm(x, residual=x.bfloat16()), "residual"), (lambda: cb.gated_norm(x.t()), "contiguous"), (lambda: cb.gated_norm(x, eps=-1.0), "eps"),
+            (lambda: cb.gated_norm(x, w8.cpu()), "expected"), (lambda: cb.gated_norm(x, scale=w8.bfloat16()), "scale"),
+            (lambda: cb.gated_norm(x, sum_out=x.bfloat16()), "sum_out"), (lambda: cb.gated_norm(torch.zeros(2, 20000, device="cuda")), "16384"),
+            (lambda: cb.QuantisedLinear(codes, scales, group=16), "group"), (lambda: cb.QuantisedLinear(codes.int(), scales), "uint8"),
+            (lambda: cb.QuantisedLinear(codes, scales.float()), "bfloat16"), (lambda: cb.QuantisedLinear(codes, scales[:5]), "shape"),
+            (lambda: cb.QuantisedLinear(codes, scales, w8), "bias"), (lambda: layer(x[:, :7]), "axis of 8"), (lambda: layer(x.half()), "float32 or"),
+            (lambda: layer(x.t().contiguous().t()), "contiguous"), (lambda: layer(x, out=x), "out"), (lambda: layer(x.cpu()), "CUDA"),
+            (lambda: cb.quantise_weights(x, 48), "group"), (lambda: cb.quantise_weights(x[0]), "matrix"),
+            (lambda: cb.LinearAttention([1.5], 8, 8), "decay"), (lambda: cb.LinearAttention([], 8, 8), "decay"), (lambda: cb.LinearAttention([float("nan")], 8, 8), "decay"),
+            (lambda: cb.LinearAttention([0.5] * 3, 8, 8, kv_heads=2), "multiple"), (lambda: cb.LinearAttention([0.5], 0, 8), "sizes"),
+            (lambda: cb.LinearAttention([0.5], 8, 8, n_streams=0), "n_streams"),
+            (lambda: att.process(q, q, k), "shape"), (lambda: att.process(q, k, k.bfloat16()), "one type"), (lambda: att.process(q[:1], k, k), "shape"),
+            (lambda: att.process(q, k, k, i[:2]), "lengths"), (lambda: att.process(q, k, k, out=k), "out"), (lambda: att.process(q.half(), k.half(), k.half()), "float32 or"),
+            (lambda: att.process(q.transpose(2, 3).contiguous().transpose(2, 3), k, k), "contiguous")):
+        with pytest.raises(cb.CBInferError, match=re.escape(message)):
+            call()
+    att.process(q, k, k)  # and what is right still runs
+    layer(x)
