@@ -4,6 +4,7 @@
 // has seen; a larger maximum m' multiplies both by exp(m - m') after t has taken (m - m') s.  Two such triples
 // join the same way, and log s - t / s is the entropy: two terms of one sign, nothing cancels.
 #include "tokens.h"
+#include <algorithm>
 
 namespace cbk {
 namespace {
@@ -27,7 +28,7 @@ __device__ __forceinline__ void add(Sums &a, float x)
 {
     const float d = x - a.m, e = __expf(d);
     a.s += e;
-    a.t += e * fmaxf(d, -200.0f); // scores of -inf: e is 0
+    a.t = __builtin_fmaf(e, fmaxf(d, -200.0f), a.t); // scores of -inf: e is 0
 }
 
 __device__ __forceinline__ void join(Sums &a, Sums b)
@@ -39,45 +40,7 @@ __device__ __forceinline__ void join(Sums &a, Sums b)
     a.t += b.t;
 }
 
-// The largest `k` of what a wave has seen, best first: lane j holds the one of rank j.  Among equal values the
-// lower index comes first.  Places not taken yet hold -inf and an index behind all others.
-struct Best {
-    float v;
-    int i;
-    float least; // of rank k - 1, the same in every lane
-    int n;       // places taken, the same in every lane
-};
-constexpr int kNone = 0x7fffffff;
-
-__device__ __forceinline__ Best best_none() { return {-__builtin_inff(), kNone, -__builtin_inff(), 0}; }
-
-__device__ __forceinline__ void insert(Best &b, int k, float x, int i)
-{
-    const int lane = threadIdx.x & 63;
-    const bool before = lane < k && (b.v > x || (b.v == x && b.i < i));
-    const int at = __popcll(__ballot(before));
-    const float pv = __shfl_up(b.v, 1);
-    const int pi = __shfl_up(b.i, 1);
-    if (lane > at) { b.v = pv; b.i = pi; }
-    if (lane == at) { b.v = x; b.i = i; }
-    b.least = __shfl(b.v, k - 1);
-    b.n = min(b.n + 1, k);
-}
-
-// What lanes hold is to be taken in lane order, which is the order of their indices: every lane whose x is larger than
-// the least of the list (a full list keeps the earlier of equals).
-__device__ __forceinline__ void offer(Best &b, int k, float x, int i, bool there)
-{
-    int from = 0;
-    for (;;) {
-        const unsigned long long m = __ballot(there && (b.n < k || x > b.least)) >> from << from;
-        if (!m) return;
-        const int l = __ffsll((long long)m) - 1;
-        insert(b, k, __shfl(x, l), __shfl(i, l));
-        if (l == 63) return;
-        from = l + 1;
-    }
-}
+constexpr int kNone = 0x7fffffff; // an index behind all others
 
 // Order of scores with NaN in front of every number.
 __device__ __forceinline__ int rank_key(float x)
@@ -86,6 +49,123 @@ __device__ __forceinline__ int rank_key(float x)
     const int b = __float_as_int(x + 0.0f);
     return b < 0 ? b ^ 0x7fffffff : b;
 }
+__device__ __forceinline__ float of_key(int key) { return __int_as_float(key < 0 ? key ^ 0x7fffffff : key); }
+
+__device__ __forceinline__ float lane_value(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
+// The value of the lane before; lane 0 keeps its own.
+__device__ __forceinline__ int from_lane_before(int v) { return __builtin_amdgcn_update_dpp(v, v, 0x138 /* wave_shr:1 */, 0xf, 0xf, false); }
+__device__ __forceinline__ int lanes_below(unsigned long long m) { return __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0)); }
+__device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
+struct Entry {
+    float v;
+    int i;
+};
+__device__ __forceinline__ bool better(const Entry &a, const Entry &b) { return a.v > b.v || (a.v == b.v && a.i < b.i); }
+
+// The k best scores of what a wave has seen: the largest, the lower index first among equals.  While it looks, a wave only
+// gathers candidates, in a buffer of 64 in LDS, against a bound that it raises now and then: keeping a list sorted score by
+// score costs more than the sums.  A buffer that runs full is worked into a list, of which lane j holds rank j.
+struct Best {
+    Entry *buffer;
+    int k, n;    // n: candidates in the buffer
+    bool listed; // whether there is a list
+    Entry mine;  // of the list
+    // the same in every lane: a score has to exceed `least`, or equal it at a lower index than `last` -- those of rank k - 1 of the
+    // list, or of a value that k of the scores at least reach, with the index behind all others
+    float least;
+    int last;
+
+    __device__ __forceinline__ void begin(Entry *b, int k_)
+    {
+        buffer = b;
+        k = k_;
+        n = 0;
+        listed = false;
+        mine = {-__builtin_inff(), kNone};
+        least = -__builtin_inff();
+        last = kNone;
+    }
+    __device__ __forceinline__ bool wanted(const Entry &e) const { return e.v > least || (e.v == least && e.i < last); }
+    // Whether any of several scores may be, `most` the largest, of higher indices than those in the list.
+    __device__ __forceinline__ bool any_wanted(float most) const { return most > least || (last == kNone && most == least); }
+    __device__ __forceinline__ void raise(float to, int at)
+    {
+        if (to > least || (to == least && at < last)) {
+            least = to;
+            last = at;
+        }
+    }
+    // A value that k of the scores at least reach, from one score a lane: close to the k-th largest of these.  What is below
+    // cannot be among the k largest.
+    __device__ __forceinline__ void bound(float most)
+    {
+        const unsigned key = (unsigned)rank_key(most) ^ 0x80000000u; // ascending as unsigned numbers
+        unsigned at = 0;
+#pragma nounroll
+        for (unsigned bit = 1u << 31; bit >= 1u << 16; bit >>= 1) // the upper half: somewhat below is a bound as well
+            if (__popcll(__ballot(key >= (at | bit))) >= k) at |= bit;
+        const float f = of_key((int)(at ^ 0x80000000u));
+        if (f == f) raise(f, kNone);
+    }
+    __device__ void flush()
+    {
+        const int lane = threadIdx.x & 63;
+        wave_fence();
+        const Entry e = lane < n ? buffer[lane] : Entry{-__builtin_inff(), kNone};
+        wave_fence();
+        if (n >= k) bound(e.v);
+        unsigned long long m = __ballot(lane < n && wanted(e));
+        while (m) {
+            const int l = __ffsll((long long)m) - 1;
+            const Entry x = {lane_value(e.v, l), __builtin_amdgcn_readlane(e.i, l)};
+            m &= m - 1;
+            if (!wanted(x)) continue;
+            const int at = __popcll(__ballot(lane < k && better(mine, x)));
+            const Entry before = {__int_as_float(from_lane_before(__float_as_int(mine.v))), from_lane_before(mine.i)};
+            mine = lane > at ? before : lane == at ? x : mine;
+            raise(lane_value(mine.v, k - 1), __builtin_amdgcn_readlane(mine.i, k - 1));
+        }
+        n = 0;
+        listed = true;
+    }
+    // One score a lane, in any order.
+    __device__ __forceinline__ void offer(const Entry &e, bool there)
+    {
+        unsigned long long m = __ballot(there && wanted(e));
+        if (!m) return;
+        if (n + __popcll(m) > 64) {
+            flush();
+            m = __ballot(there && wanted(e));
+        }
+        if (m >> (threadIdx.x & 63) & 1) buffer[n + lanes_below(m)] = e;
+        n += __popcll(m);
+    }
+    // Nothing more comes: at most 64 candidates in the buffer, those of the list included.
+    __device__ __forceinline__ void settle()
+    {
+        if (listed) {
+            flush();
+            const unsigned long long m = __ballot((threadIdx.x & 63) < (unsigned)k && mine.i != kNone);
+            if (m >> (threadIdx.x & 63) & 1) buffer[threadIdx.x & 63] = mine;
+            n = __popcll(m);
+        }
+        wave_fence();
+    }
+    // Behind settle(): every candidate's rank among them; k and more, or the lane holds none: not among the best.
+    __device__ __forceinline__ int ranked(Entry &e) const
+    {
+        const int lane = threadIdx.x & 63;
+        e = lane < n ? buffer[lane] : Entry{-__builtin_inff(), kNone};
+        int rank = lane < n ? 0 : 64;
+#pragma nounroll
+        for (int l = 0; l < n; ++l) {
+            const Entry o = {lane_value(e.v, l), __builtin_amdgcn_readlane(e.i, l)};
+            rank += better(o, e);
+        }
+        return rank;
+    }
+};
 
 template <int DT>
 __device__ __forceinline__ float score(const cbinfer_log_probs_args &a, int64_t at)
@@ -124,65 +204,488 @@ __device__ __forceinline__ float log_prob(float x, const Sums &t, float log_s)
     return t.s != t.s ? __builtin_nanf("") : t.s == 0.0f ? -__builtin_inff() : (x - t.m) - log_s;
 }
 
-// Label and entropy of a position from its sums: lane-wise work, `scores` at its base.
+// What a position's label asks for, read before the scores are: two dependent loads, whose time would otherwise come on top.
+struct Label {
+    int64_t l;
+    float x;
+};
 template <int DT>
-__device__ __forceinline__ void write_position(const cbinfer_log_probs_args &a, int64_t pos, int64_t base, const Sums &t, float log_s)
+__device__ __forceinline__ Label read_label(const cbinfer_log_probs_args &a, int64_t pos, int64_t base)
+{
+    Label r = {-1, 0.0f};
+    if (!a.label) return r;
+    r.l = a.label_bytes == 8 ? static_cast<const int64_t *>(a.labels)[pos] : static_cast<const int32_t *>(a.labels)[pos];
+    if (r.l >= 0 && r.l < a.classes) r.x = score<DT>(a, base + r.l * a.class_stride);
+    return r;
+}
+
+// Label and entropy of a position from its sums.
+__device__ __forceinline__ void write_position(const cbinfer_log_probs_args &a, int64_t pos, const Label &label, const Sums &t, float log_s)
 {
     if (a.entropy) a.entropy[pos] = t.s != t.s ? __builtin_nanf("") : t.s == 0.0f ? 0.0f : log_s - t.t / t.s;
-    if (a.label) {
-        const int64_t l = a.label_bytes == 8 ? static_cast<const int64_t *>(a.labels)[pos] : static_cast<const int32_t *>(a.labels)[pos];
-        float v = 0.0f;
-        if (l >= a.classes)
-            v = __builtin_nanf("");
-        else if (l >= 0)
-            v = log_prob(score<DT>(a, base + l * a.class_stride), t, log_s);
-        a.label[pos] = v;
+    if (a.label)
+        a.label[pos] = label.l < 0 ? 0.0f : label.l >= a.classes ? __builtin_nanf("") : log_prob(label.x, t, log_s);
+}
+
+// Sums of a wave, in every lane.
+__device__ __forceinline__ void join_lanes(Sums &t)
+{
+    for (int off = 32; off; off >>= 1) join(t, {__shfl_xor(t.m, off), __shfl_xor(t.s, off), __shfl_xor(t.t, off)});
+}
+
+// Everything of a position from the sums and the list of the whole row, by one wave.
+template <int DT>
+__device__ void finish(const cbinfer_log_probs_args &a, int64_t pos, int64_t base, int64_t to, const Label &label, const Sums &t, Best &b)
+{
+    const int lane = threadIdx.x & 63;
+    const float log_s = logf(t.s);
+    if (lane == 0) write_position(a, pos, label, t, log_s);
+    if (!a.top) return;
+    if (t.s != t.s) {
+        careful_top<DT>(a, base, to);
+        return;
+    }
+    Entry e;
+    const int rank = b.ranked(e);
+    if (rank < a.top) {
+        a.top_values[to + rank * a.inner] = log_prob(e.v, t, log_s);
+        a.top_index[to + rank * a.inner] = e.i;
     }
 }
 
 // One wave a position, any strides.
 template <int DT>
-__global__ __launch_bounds__(256) void wave_kernel(const cbinfer_log_probs_args a)
+__global__ __launch_bounds__(256) void wave_kernel(const cbinfer_log_probs_args a, int64_t first, FastDiv inner)
 {
     const int lane = threadIdx.x & 63;
-    const int64_t pos = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t pos = first + (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (pos >= a.outer * a.inner) return;
-    const int64_t o = pos / a.inner, i = pos - o * a.inner;
+    const int64_t o = fast_div((int)pos, inner), i = pos - o * a.inner;
     const int64_t base = o * a.outer_stride + i * a.inner_stride, to = o * a.top * a.inner + i;
+    __shared__ Entry buffers[4][64];
+    const Label label = read_label<DT>(a, pos, base);
     Sums t = {kLowest, 0.0f, 0.0f};
-    Best b = best_none();
+    Best b;
+    b.begin(buffers[threadIdx.x >> 6], a.top);
     for (int64_t c0 = 0; c0 < a.classes; c0 += 64) {
         const int64_t c = c0 + lane;
         const bool there = c < a.classes;
         const float x = there ? score<DT>(a, base + c * a.class_stride) : -__builtin_inff();
         if (x > t.m) raise_to(t, x);
         add(t, x);
-        if (a.top) offer(b, a.top, x, (int)c, there);
+        if (a.top) b.offer({x, (int)c}, there);
     }
-    for (int off = 32; off; off >>= 1) join(t, {__shfl_xor(t.m, off), __shfl_xor(t.s, off), __shfl_xor(t.t, off)});
+    if (a.top) b.settle();
+    join_lanes(t);
+    finish<DT>(a, pos, base, to, label, t, b);
+}
+
+// ---- classes behind one another ----------------------------------------------------------------
+template <int DT>
+struct Row {
+    static constexpr int V = DT == kF32 ? 4 : 8; // scores in 16 bytes
+    static __device__ __forceinline__ void unpack(const uint4 &u, float (&x)[V])
+    {
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[e] = Unit<DT>::get(u, e);
+    }
+};
+
+// What a workgroup that shares a row leaves of it: the sums, then `top` entries, best first.
+inline __host__ __device__ int segment_floats(int top) { return 3 + 2 * top; }
+
+// `WAVES` waves of a workgroup take a row, or with several segments a row their part of it.  A wave loads 16 bytes a lane, U
+// times over before it uses them; rows may begin at any address: the scores in front of the first 16-byte boundary and
+// behind the last one are taken one by one.
+template <int DT, int WAVES, int U>
+__global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void rows_kernel(const cbinfer_log_probs_args a, int64_t first_row, FastDiv inner, int segments, float *found)
+{
+    typedef typename Elem<DT>::type T;
+    constexpr int V = Row<DT>::V, ROWS = WAVES < 4 ? 4 / WAVES : 1, NT = WAVES * 64;
+    __shared__ float shared[WAVES > 1 ? NT : 1];
+    __shared__ Entry buffers[WAVES < 4 ? 4 : WAVES][64];
+    __shared__ int counts[WAVES];
+    const int lane = threadIdx.x & 63, wave = (threadIdx.x >> 6) % WAVES, thread = threadIdx.x % NT;
+    const int64_t row = first_row + (int64_t)blockIdx.x * ROWS + (WAVES < 4 ? threadIdx.x / NT : 0);
+    if (ROWS > 1 && row >= a.outer * a.inner) return; // a whole wave, and WAVES is 1 then
+    const int segment = blockIdx.y;
+    const int64_t o = fast_div((int)row, inner), in = row - o * a.inner, base = o * a.outer_stride + in * a.inner_stride;
+    const T *x = static_cast<const T *>(a.scores) + base;
+    const int n = (int)a.classes, k = a.top;
+    const int head = min(n, (int)(-(reinterpret_cast<uintptr_t>(x) / sizeof(T)) & (V - 1))), units = (n - head) / V, tail = head + units * V;
+    const int per = (units + segments - 1) / segments, end = min(units, (segment + 1) * per);
+    const uint4 *body = reinterpret_cast<const uint4 *>(x + head);
+    const Label label = segments == 1 ? read_label<DT>(a, row, base) : Label{-1, 0.0f};
+
+    Sums t = {kLowest, 0.0f, 0.0f};
+    Best b;
+    b.begin(buffers[threadIdx.x >> 6], k);
+    auto few = [&](int from, int to) { // fewer than 64, by the first wave
+        if (from >= to || wave != 0) return;
+        const bool there = from + lane < to;
+        const float v = there ? Elem<DT>::get(x[from + lane]) : -__builtin_inff();
+        if (v > t.m) raise_to(t, v);
+        add(t, v);
+        if (k) b.offer({v, from + lane}, there);
+    };
+    if (segment == 0) few(0, head);
+    uint4 next[U];
+    auto load = [&](int u0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int at = u0 + u * NT + thread;
+            const unsigned none = DT == kF32 ? 0xff800000u : 0xff80ff80u; // -inf
+            next[u] = make_uint4(none, none, none, none);
+            if (at < end) next[u] = body[at];
+        }
+    };
+    load(segment * per);
+    int again = 0, round = 0;
+#pragma nounroll
+    for (int u0 = segment * per; u0 < end; u0 += U * NT, ++round) {
+        uint4 raw[U];
+        float largest[U], most;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            raw[u] = next[u];
+            float v[V];
+            Row<DT>::unpack(raw[u], v);
+            largest[u] = v[0];
+#pragma unroll
+            for (int e = 1; e < V; ++e) largest[u] = fmaxf(largest[u], v[e]);
+            most = u ? fmaxf(most, largest[u]) : largest[u];
+        }
+        load(u0 + U * NT);
+        raise_to(t, fmaxf(t.m, most));
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float v[V];
+            Row<DT>::unpack(raw[u], v);
+#pragma unroll
+            for (int e = 0; e < V; ++e) add(t, v[e]);
+        }
+        if (!k) continue;
+        if (round == again) { // rounds 0, 3, 15, 63, ...: what a round wants in the mean falls with the scores that the bound has seen
+            again = 4 * again + 3;
+            float top = t.m == kLowest ? most : t.m; // the largest so far; of scores of -inf t.m says nothing
+            if (WAVES > 1) {
+                shared[threadIdx.x] = top;
+                __syncthreads();
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) top = fmaxf(top, shared[w * 64 + lane]);
+                __syncthreads();
+            }
+            b.bound(top);
+        }
+        const unsigned long long hit = __ballot(b.any_wanted(most));
+        if (!hit) continue;
+        if (__popcll(hit) > 32) b.bound(most); // scores that rise
+#pragma nounroll
+        for (int u = 0; u < U; ++u) { // one place in the code: the units move past it
+            unsigned long long m = __ballot(b.any_wanted(largest[0]) && u0 + u * NT + thread < end);
+            while (m) { // a lane's unit, a score a lane
+                const int l = __ffsll((long long)m) - 1;
+                m &= m - 1;
+                uint4 unit;
+                unit.x = __builtin_amdgcn_readlane(raw[0].x, l);
+                unit.y = __builtin_amdgcn_readlane(raw[0].y, l);
+                unit.z = __builtin_amdgcn_readlane(raw[0].z, l);
+                unit.w = __builtin_amdgcn_readlane(raw[0].w, l);
+                const int word = lane / (V / 4);
+                const unsigned w = word == 0 ? unit.x : word == 1 ? unit.y : word == 2 ? unit.z : unit.w;
+                const float x = __uint_as_float(DT == kF32 ? w : lane & 1 ? w & 0xffff0000u : w << 16);
+                b.offer({x, head + (u0 + u * NT + thread - lane + l) * V + lane}, lane < V);
+            }
+#pragma unroll
+            for (int j = 0; j + 1 < U; ++j) {
+                raw[j] = raw[j + 1];
+                largest[j] = largest[j + 1];
+            }
+        }
+    }
+    if (segment == segments - 1) few(tail, n);
+    if (k) b.settle();
+    join_lanes(t);
+    if (WAVES > 1) {
+        if (lane == 0) {
+            shared[wave * 3] = t.m; shared[wave * 3 + 1] = t.s; shared[wave * 3 + 2] = t.t;
+            counts[wave] = b.n;
+        }
+        __syncthreads();
+        if (wave != 0) return;
+        t = {kLowest, 0.0f, 0.0f};
+        if (lane < WAVES) t = {shared[lane * 3], shared[lane * 3 + 1], shared[lane * 3 + 2]};
+        join_lanes(t);
+        if (k) { // the first wave's buffer is read before it is used again
+            Entry e[WAVES];
+            float most = -__builtin_inff();
+            int all = 0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                e[w] = lane < counts[w] ? buffers[w][lane] : Entry{-__builtin_inff(), kNone};
+                most = fmaxf(most, e[w].v);
+                all += counts[w];
+            }
+            wave_fence();
+            const float least = b.least;
+            b.begin(buffers[0], k);
+            b.raise(least, kNone);
+            if (all > 2 * k) b.bound(most);
+#pragma nounroll
+            for (int w = 0; w < WAVES; ++w) {
+                b.offer(e[0], lane < counts[w]);
+#pragma unroll
+                for (int j = 0; j + 1 < WAVES; ++j) e[j] = e[j + 1];
+            }
+            b.settle();
+        }
+    }
+    if (segments == 1) {
+        finish<DT>(a, row, base, o * a.top * a.inner + in, label, t, b);
+    } else {
+        float *mine = found + (row * segments + segment) * segment_floats(k);
+        if (lane == 0) { mine[0] = t.m; mine[1] = t.s; mine[2] = t.t; }
+        if (k) {
+            Entry e;
+            const int rank = b.ranked(e);
+            if (rank < k) { mine[3 + rank] = e.v; mine[3 + k + rank] = __int_as_float(e.i); }
+            if (lane >= b.n && lane < k) { mine[3 + lane] = -__builtin_inff(); mine[3 + k + lane] = __int_as_float(kNone); }
+        }
+    }
+}
+
+// The segments of a row, a wave a row.
+template <int DT>
+__global__ __launch_bounds__(256) void join_kernel(const cbinfer_log_probs_args a, int64_t first, FastDiv inner, int segments, const float *found)
+{
+    __shared__ Entry buffers[4][64];
+    const int lane = threadIdx.x & 63, k = a.top, each = segment_floats(k);
+    const int64_t row = first + (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= a.outer * a.inner) return;
+    const int64_t o = fast_div((int)row, inner), in = row - o * a.inner;
+    found += row * segments * each;
+    const int64_t base = o * a.outer_stride + in * a.inner_stride;
+    const Label label = read_label<DT>(a, row, base);
+    Sums t = {kLowest, 0.0f, 0.0f};
+    float best = -__builtin_inff(), least = best; // of a segment: below the least of k a score has k better ones, ...
+    if (lane < segments) {
+        t = {found[lane * each], found[lane * each + 1], found[lane * each + 2]};
+        if (k) {
+            best = found[lane * each + 3];
+            least = found[lane * each + 3 + k - 1];
+        }
+    }
+    join_lanes(t);
+    Best b;
+    b.begin(buffers[threadIdx.x >> 6], k);
+    if (k) {
+        for (int off = 32; off; off >>= 1) least = fmaxf(least, __shfl_xor(least, off));
+        b.raise(least, kNone);
+        if (segments >= k) b.bound(best); // ... and below the k-th largest of the segments' best too
+        for (int at = lane; at - lane < segments * k; at += 64) {
+            const bool there = at < segments * k;
+            const int list = there ? at / k : 0, j = there ? at - list * k : 0;
+            b.offer({found[list * each + 3 + j], __float_as_int(found[list * each + 3 + k + j])}, there);
+        }
+        b.settle();
+    }
+    finish<DT>(a, row, base, o * a.top * a.inner + in, label, t, b);
+}
+
+// ---- positions behind one another: maps ------------------------------------------------------------
+// A lane takes a position and keeps its K best in registers, best first.
+template <int K>
+struct Ranked {
+    float v[K ? K : 1];
+    int i[K ? K : 1];
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int j = 0; j < K; ++j) { v[j] = -__builtin_inff(); i[j] = kNone; }
+    }
+    // NaN is never taken: rows that hold one are ranked again.
+    __device__ __forceinline__ void insert(float x, int c)
+    {
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            const bool better = x > v[j] || (x == v[j] && c < i[j]);
+            const float ov = v[j];
+            const int oi = i[j];
+            v[j] = better ? x : ov;
+            i[j] = better ? c : oi;
+            x = better ? ov : x;
+            c = better ? oi : c;
+        }
+    }
+    __device__ __forceinline__ bool wants(float x) const { return K && (x > v[K ? K - 1 : 0] || i[K ? K - 1 : 0] == kNone); }
+};
+
+// careful_top for a lane by itself.
+template <int DT>
+__device__ void careful_top_lane(const cbinfer_log_probs_args &a, int64_t base, int64_t to)
+{
+    int key = kNone, index = -1;
+    for (int j = 0; j < a.top; ++j) {
+        int bk = -kNone - 1, bi = kNone;
+        for (int c = 0; c < (int)a.classes; ++c) {
+            const int k = rank_key(score<DT>(a, base + c * a.class_stride));
+            const bool behind = j == 0 || k < key || (k == key && c > index);
+            if (behind && k > bk) { bk = k; bi = c; }
+        }
+        key = bk;
+        index = bi;
+        a.top_values[to + j * a.inner] = __builtin_nanf("");
+        a.top_index[to + j * a.inner] = bi;
+    }
+}
+
+// PARTS > 1: the waves of a workgroup share the classes of 256 / PARTS positions, for maps that would not fill the chip
+// otherwise.  CH classes are loaded before they are used.
+template <int DT, int K, int PARTS>
+__global__ __launch_bounds__(256) void map_kernel(const cbinfer_log_probs_args a, FastDiv inner)
+{
+    constexpr int CH = 8, NP = 256 / PARTS;
+    typedef typename Elem<DT>::type T;
+    __shared__ float sums[PARTS > 1 ? PARTS - 1 : 1][3 + 2 * K][PARTS > 1 ? NP : 1];
+    const int part = threadIdx.x / NP, place = threadIdx.x % NP;
+    const int64_t pos = (int64_t)blockIdx.x * NP + place;
+    const bool there = pos < a.outer * a.inner;
+    const int o = there ? fast_div((int)pos, inner) : 0;
+    const int64_t i = there ? pos - (int64_t)o * a.inner : 0, base = o * a.outer_stride + i * a.inner_stride;
+    const T *x = static_cast<const T *>(a.scores) + base;
+    const Label label = there && part == 0 ? read_label<DT>(a, pos, base) : Label{-1, 0.0f};
+    const int n = (int)a.classes, each = (n + PARTS - 1) / PARTS, end = min(n, (part + 1) * each);
+    Sums t = {kLowest, 0.0f, 0.0f};
+    Ranked<K> b;
+    b.clear();
+    if (there) {
+        for (int c0 = part * each; c0 < end; c0 += CH) {
+            float v[CH], most = kLowest;
+#pragma unroll
+            for (int e = 0; e < CH; ++e) {
+                v[e] = c0 + e < end ? Elem<DT>::get(x[(c0 + e) * a.class_stride]) : -__builtin_inff();
+                most = fmaxf(most, v[e]);
+            }
+            raise_to(t, fmaxf(t.m, most));
+#pragma unroll
+            for (int e = 0; e < CH; ++e) add(t, v[e]);
+            if (b.wants(most)) {
+#pragma unroll
+                for (int e = 0; e < CH; ++e)
+                    if (c0 + e < end && b.wants(v[e])) b.insert(v[e], c0 + e);
+            }
+        }
+    }
+    if (PARTS > 1) {
+        if (part) {
+            float (*mine)[PARTS > 1 ? NP : 1] = sums[part - 1];
+            mine[0][place] = t.m; mine[1][place] = t.s; mine[2][place] = t.t;
+#pragma unroll
+            for (int j = 0; j < K; ++j) { mine[3 + j][place] = b.v[j]; mine[3 + K + j][place] = __int_as_float(b.i[j]); }
+        }
+        __syncthreads();
+        if (part) return;
+        for (int p = 0; p + 1 < PARTS; ++p) { // ascending classes
+            join(t, {sums[p][0][place], sums[p][1][place], sums[p][2][place]});
+#pragma unroll
+            for (int j = 0; j < K; ++j) {
+                const float v = sums[p][3 + j][place];
+                const int c = __float_as_int(sums[p][3 + K + j][place]);
+                if (c != kNone && b.wants(v)) b.insert(v, c);
+            }
+        }
+    }
+    if (!there) return;
     const float log_s = logf(t.s);
-    if (lane == 0) write_position<DT>(a, pos, base, t, log_s);
-    if (!a.top) return;
+    write_position(a, pos, label, t, log_s);
+    if (!K) return;
+    const int64_t to = (int64_t)o * a.top * a.inner + i;
     if (t.s != t.s) {
-        careful_top<DT>(a, base, to);
-    } else if (lane < a.top) {
-        a.top_values[to + lane * a.inner] = log_prob(b.v, t, log_s);
-        a.top_index[to + lane * a.inner] = b.i;
+        careful_top_lane<DT>(a, base, to);
+        return;
     }
+#pragma unroll
+    for (int j = 0; j < K; ++j)
+        if (j < a.top) {
+            a.top_values[to + j * a.inner] = log_prob(b.v[j], t, log_s);
+            a.top_index[to + j * a.inner] = b.i[j];
+        }
+}
+
+template <int DT, int PARTS>
+hipError_t map_any(hipStream_t st, const cbinfer_log_probs_args &a)
+{
+    const unsigned grid = (unsigned)((a.outer * a.inner + 256 / PARTS - 1) / (256 / PARTS));
+    const FastDiv inner = make_fastdiv((int)a.inner);
+    auto kernel = a.top == 0 ? map_kernel<DT, 0, PARTS> : a.top == 1 ? map_kernel<DT, 1, PARTS> : a.top <= 4 ? map_kernel<DT, 4, PARTS> :
+                  a.top <= 8 ? map_kernel<DT, 8, PARTS> : map_kernel<DT, 16, PARTS>;
+    kernel<<<grid, 256, 0, st>>>(a, inner);
+    return hipGetLastError();
 }
 
 } // namespace
+namespace {
+enum { kAnyStride, kRows, kMaps };
+struct Plan {
+    int kind, waves, segments;
+};
 
-size_t log_probs_workspace(const cbinfer_log_probs_args &) { return 0; }
-
-hipError_t log_probs(hipStream_t st, const cbinfer_log_probs_args &a)
+Plan plan(const cbinfer_log_probs_args &a)
 {
-    const unsigned blocks = (unsigned)((a.outer * a.inner + 3) / 4);
-    if (a.dtype == kF32)
-        wave_kernel<kF32><<<blocks, 256, 0, st>>>(a);
-    else
-        wave_kernel<kBF16><<<blocks, 256, 0, st>>>(a);
-    return hipGetLastError();
+    Plan p = {kAnyStride, 1, 1};
+    const int64_t positions = a.outer * a.inner;
+    if (a.class_stride == 1) {
+        p.kind = kRows;
+        // us a call, 4096 rows of 1000 bfloat16: a wave each 17, four waves each 32
+        if (a.classes <= 2048) return p;
+        p.waves = 4;
+        // Few long rows are cut into segments of one round of loads at least, up to 1024 workgroups, and joined by a second launch.
+        // 64 rows of 100003 bfloat16: 29 us whole, 18 in 12 segments and more, join included; one of 131071: 28 and 18.
+        const int64_t rounds = a.classes / (4 * 64 * 4 * (a.dtype == kF32 ? 4 : 8)), segments = std::min<int64_t>({rounds, 64, 1024 / std::max<int64_t>(positions, 1)});
+        if (segments >= 4) p.segments = (int)segments;
+    } else if (a.inner_stride == 1 && a.inner >= 16 && a.top <= 16 && (a.classes <= 1024 || positions >= 16384)) {
+        p.kind = kMaps;
+        p.waves = positions < 65536 && a.classes >= 32 ? 4 : 1;
+    }
+    return p;
 }
+
+constexpr int64_t kMostBlocks = 1 << 20; // of a launch: threads are counted in 32 bits
+
+template <int DT>
+hipError_t run(hipStream_t st, const cbinfer_log_probs_args &a)
+{
+    const Plan p = plan(a);
+    const int64_t positions = a.outer * a.inner;
+    if (p.kind == kMaps) return p.waves == 4 ? map_any<DT, 4>(st, a) : map_any<DT, 1>(st, a);
+    float *found = static_cast<float *>(a.workspace);
+    const FastDiv inner = make_fastdiv((int)a.inner);
+    const int per_block = p.kind == kRows && p.waves > 1 ? 1 : 4;
+    for (int64_t first = 0; first < positions; first += kMostBlocks * per_block) {
+        const unsigned blocks = (unsigned)std::min(kMostBlocks, (positions - first + per_block - 1) / per_block);
+        const dim3 grid(blocks, p.segments);
+        if (p.kind != kRows)
+            wave_kernel<DT><<<blocks, 256, 0, st>>>(a, first, inner);
+        else if (p.waves == 1)
+            rows_kernel<DT, 1, 4><<<grid, 256, 0, st>>>(a, first, inner, p.segments, found);
+        else
+            rows_kernel<DT, 4, 4><<<grid, 256, 0, st>>>(a, first, inner, p.segments, found);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    if (p.segments > 1) {
+        join_kernel<DT><<<(unsigned)((positions + 3) / 4), 256, 0, st>>>(a, 0, inner, p.segments, found);
+        return hipGetLastError();
+    }
+    return hipSuccess;
+}
+} // namespace
+
+size_t log_probs_workspace(const cbinfer_log_probs_args &a)
+{
+    const Plan p = plan(a);
+    return p.segments > 1 ? (size_t)(a.outer * a.inner) * p.segments * segment_floats(a.top) * sizeof(float) : 0;
+}
+
+hipError_t log_probs(hipStream_t st, const cbinfer_log_probs_args &a) { return a.dtype == kF32 ? run<kF32>(st, a) : run<kBF16>(st, a); }
 
 } // namespace cbk

@@ -65,8 +65,8 @@ int check(const cbinfer_linear_attention_args *a)
     if (a->key_size < 1 || a->key_size > 256 || a->value_size < 1 || a->value_size > 256)
         return refuse(CBINFER_EUNSUPPORTED, "%s: key and value sizes must be 1 .. 256 (got %d and %d)", w, a->key_size,
                       a->value_size);
-    if ((int64_t)a->streams * a->heads > (1 << 24))
-        return refuse(CBINFER_EUNSUPPORTED, "%s: streams times heads must be at most 2^24", w);
+    if ((int64_t)a->streams * a->heads > (1 << 18))
+        return refuse(CBINFER_EUNSUPPORTED, "%s: streams times heads must be at most 2^18", w);
     if (!std::isfinite(a->scale)) return refuse(CBINFER_EINVAL, "%s: scale must be finite", w);
     return CBINFER_OK;
 }
@@ -144,8 +144,9 @@ int cbinfer_quantise_weights(const void *weights, int32_t dtype, int64_t rows, i
 
 size_t cbinfer_packed_weights_bytes(int64_t rows, int64_t cols, int32_t group)
 {
-    if (rows < 1 || cols < 1 || rows > (1 << 28) || cols > (1 << 28)) {
-        refuse(CBINFER_EINVAL, "4-bit weights: rows and cols must be 1 .. 2^28");
+    // threads of a launch are counted in 32 bits
+    if (rows < 1 || cols < 1 || rows > (1 << 26) || cols > (1 << 26) || rows * cols > (int64_t)1 << 32) {
+        refuse(CBINFER_EINVAL, "4-bit weights: rows and cols must be 1 .. 2^26, together at most 2^32");
         return 0;
     }
     if (group != 32 && group != 64 && group != 128) {

@@ -9,6 +9,8 @@ from __future__ import annotations
 import ctypes as C
 from typing import NamedTuple, Optional, Sequence
 
+import torch
+
 from .binding import BF16, F32, CBInferError, _last_error, load_library
 
 GATES = {None: 0, "silu": 1, "sigmoid": 2}
@@ -85,25 +87,26 @@ def _refuse(message: str):
     raise CBInferError(EINVAL, message)
 
 
+_KINDS = {torch.float32: F32, torch.bfloat16: BF16}
+
+
 def _dtype(t, what: str) -> int:
-    import torch
-    if t.dtype == torch.float32:
-        return F32
-    if t.dtype == torch.bfloat16:
-        return BF16
-    _refuse("%s must be float32 or bfloat16 (got %s)" % (what, t.dtype))
+    kind = _KINDS.get(t.dtype)
+    if kind is None:
+        _refuse("%s must be float32 or bfloat16 (got %s)" % (what, t.dtype))
+    return kind
 
 
 def _device(t, what: str):
     """The tensor's device, which has to be the current one: kernels are launched there."""
-    import torch
     if not t.is_cuda:
         if not torch.cuda.is_available():
             raise CBInferError(EDEVICE, "no GPU visible to torch; the HIP path has no CPU fallback")
         _refuse("%s must be a CUDA tensor" % what)
-    if t.get_device() != torch.cuda.current_device():
-        _refuse("%s is on %s, the current device is %d" % (what, t.device, torch.cuda.current_device()))
-    return t.device
+    device = t.device
+    if device.index != torch._C._cuda_getDevice():
+        _refuse("%s is on %s, the current device is %d" % (what, device, torch.cuda.current_device()))
+    return device
 
 
 def _same_device(t, device, what: str):
@@ -112,20 +115,18 @@ def _same_device(t, device, what: str):
 
 
 def _float32(t, device, size: int, what: str):
-    import torch
     if t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != size or not t.is_contiguous():
         _refuse("%s must be a contiguous float32 tensor of %d values" % (what, size))
     _same_device(t, device, what)
 
 
-def _stream() -> int:
-    import torch
-    return torch.cuda.current_stream().cuda_stream
+def _stream(device) -> int:
+    """torch.cuda.current_stream(device).cuda_stream without the objects in between, which cost more than a launch."""
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _workspace(args, needed: int, device):
     """Allocated on the current stream; the caller keeps it until the launch."""
-    import torch
     if not needed:
         return None
     w = torch.empty(needed + 256, dtype=torch.uint8, device=device)
@@ -176,7 +177,6 @@ def log_probs(scores, labels=None, *, dim: int = 1, top: int = 0) -> LogProbs:
     """Log probability of `labels` (int32 or int64, the shape of scores without `dim`, or None), entropy, and the
     `top` classes with their log probabilities of float32 or bfloat16 scores of any strides whose classes lie along
     `dim`: the network's [streams][classes][H][W], or [rows][classes] of a vocabulary."""
-    import torch
     lib = _library()
     shape, strides, axes = scores.shape, scores.stride(), scores.dim()
     if axes < 1 or not -axes <= dim < axes:
@@ -214,7 +214,7 @@ def log_probs(scores, labels=None, *, dim: int = 1, top: int = 0) -> LogProbs:
         index = torch.empty(rest[:cut] + (top,) + rest[cut:], dtype=torch.int32, device=device)
         a.top_values, a.top_index = values.data_ptr(), index.data_ptr()
     keep = _workspace(a, lib.cbinfer_log_probs_workspace_bytes(a), device)  # noqa: F841
-    rc = lib.cbinfer_log_probs(a, _stream())
+    rc = lib.cbinfer_log_probs(a, _stream(device))
     if rc:
         _raise(rc)
     if top and cut != dim:
@@ -230,7 +230,6 @@ class LinearAttention:
 
     def __init__(self, decay: Sequence[float], key_size: int, value_size: int, *, n_streams: int = 1,
                  kv_heads: Optional[int] = None, scale: float = 1.0):
-        import torch
         self.lib = _library()
         if not torch.cuda.is_available():
             raise CBInferError(EDEVICE, "no GPU visible to torch; the HIP path has no CPU fallback")
@@ -266,7 +265,6 @@ class LinearAttention:
         """The next tokens of every stream: q [n_streams][tokens][heads][key_size], k [..][kv_heads][key_size],
         v [..][kv_heads][value_size], the last axis contiguous; lengths: None, or int32 [n_streams], how many of the
         tokens a stream has.  Returns [n_streams][tokens][heads][value_size] and leaves the new state."""
-        import torch
         a = linear_attention_args.from_buffer_copy(self._args)
         if q.dim() != 4:
             _refuse("q must be [streams][tokens][heads][key_size]")
@@ -298,7 +296,7 @@ class LinearAttention:
         a.q, a.k, a.v, a.o = q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr()
         a.lengths = None if lengths is None else lengths.data_ptr()
         keep = _workspace(a, self.lib.cbinfer_linear_attention_workspace_bytes(a), device)  # noqa: F841
-        rc = self.lib.cbinfer_linear_attention(a, _stream())
+        rc = self.lib.cbinfer_linear_attention(a, _stream(device))
         if rc:
             _raise(rc)
         return out
@@ -308,7 +306,6 @@ class LinearAttention:
 def quantise_weights(weight, group: int = 64):
     """Codes (uint8 [rows][cols]) and scales (bfloat16 [rows][groups]) of a float matrix, each weight the nearest
     of the 16 values under the scale of its group."""
-    import torch
     lib = _library()
     if weight.dim() != 2 or (weight.shape[1] > 1 and weight.stride(1) != 1):
         _refuse("weight must be a matrix with contiguous rows")
@@ -319,7 +316,7 @@ def quantise_weights(weight, group: int = 64):
     codes = torch.empty((rows, cols), dtype=torch.uint8, device=device)
     scales = torch.empty((rows, -(-cols // group)), dtype=torch.bfloat16, device=device)
     rc = lib.cbinfer_quantise_weights(weight.data_ptr(), kind, rows, cols, weight.stride(0), group, codes.data_ptr(),
-                                      scales.data_ptr(), _stream())
+                                      scales.data_ptr(), _stream(device))
     if rc:
         _raise(rc)
     return codes, scales
@@ -331,7 +328,6 @@ class QuantisedLinear:
     once, at construction; codes and scales are not needed afterwards."""
 
     def __init__(self, codes, scales, bias=None, *, group: int = 64):
-        import torch
         self.lib = _library()
         if codes.dim() != 2 or codes.dtype != torch.uint8 or not codes.is_contiguous():
             _refuse("codes must be a contiguous uint8 matrix")
@@ -350,7 +346,7 @@ class QuantisedLinear:
         self.bias = bias
         self._memory = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
         packed = (self._memory.data_ptr() + 255) // 256 * 256
-        rc = self.lib.cbinfer_pack_weights(codes.data_ptr(), scales.data_ptr(), self.rows, self.cols, self.group, packed, _stream())
+        rc = self.lib.cbinfer_pack_weights(codes.data_ptr(), scales.data_ptr(), self.rows, self.cols, self.group, packed, _stream(device))
         if rc:
             _raise(rc)
         a = self._args = quantised_product_args()
@@ -364,7 +360,6 @@ class QuantisedLinear:
 
     def __call__(self, x, out=None):
         """x [..][cols] float32 or bfloat16 -> [..][rows] of the same type.  Rows of x may lie apart, not their values."""
-        import torch
         a = quantised_product_args.from_buffer_copy(self._args)
         if x.dim() < 1 or x.shape[-1] != self.cols:
             _refuse("x must end in an axis of %d values (got %s)" % (self.cols, tuple(x.shape)))
@@ -382,7 +377,7 @@ class QuantisedLinear:
         a.y_stride = self.rows
         a.x, a.y = x.data_ptr(), out.data_ptr()
         keep = _workspace(a, self.lib.cbinfer_quantised_product_workspace_bytes(a), device)  # noqa: F841
-        rc = self.lib.cbinfer_quantised_product(a, _stream())
+        rc = self.lib.cbinfer_quantised_product(a, _stream(device))
         if rc:
             _raise(rc)
         return out
@@ -413,7 +408,6 @@ def gated_norm(x, weight=None, *, group: int = 0, gate=None, activation: Optiona
     h = residual + scale * u (scale: a number, or float32 per channel); y = h / rms(h) * next_weight.
     Rows along the last axis; parts that are None are left out.  Returns (h, y): h has the type of the residual
     (float32 or that of x), y (None without next_weight) that of x.  sum_out: where h goes, e.g. the residual itself."""
-    import torch
     lib = _library()
     a = gated_norm_args()
     size = x.shape[-1] if x.dim() else 0
@@ -466,7 +460,7 @@ def gated_norm(x, weight=None, *, group: int = 0, gate=None, activation: Optiona
         y = torch.empty(shape, dtype=kind, device=device)
         a.y_stride = size
         a.next_weight, a.y = next_weight.data_ptr(), y.data_ptr()
-    rc = lib.cbinfer_gated_norm(a, _stream())
+    rc = lib.cbinfer_gated_norm(a, _stream(device))
     if rc:
         _raise(rc)
     return h, y
