@@ -67,6 +67,7 @@ int check(const cbinfer_linear_attention_args *a)
                       a->value_size);
     if ((int64_t)a->streams * a->heads > (1 << 18))
         return refuse(CBINFER_EUNSUPPORTED, "%s: streams times heads must be at most 2^18", w);
+    if (a->tokens > (1 << 28)) return refuse(CBINFER_EUNSUPPORTED, "%s: tokens must be at most 2^28", w);
     if (!std::isfinite(a->scale)) return refuse(CBINFER_EINVAL, "%s: scale must be finite", w);
     return CBINFER_OK;
 }

@@ -61,7 +61,7 @@ def test_log_probs_refuses(changes, message):
     (dict(dtype=-1), "dtype"), (dict(streams=-1), ">= 0"), (dict(tokens=-1), ">= 0"), (dict(kv_heads=0), "multiple"), (dict(kv_heads=3), "multiple"),
     (dict(key_size=0), "1 .. 256"), (dict(value_size=257), "1 .. 256"), (dict(scale=float("inf")), "scale"), (dict(q=None), "q, k, v"),
     (dict(o=65), "q, k, v"), (dict(state=None), "state"), (dict(decay=66), "state and decay"), (dict(lengths=66), "lengths"),
-    (dict(streams=1 << 20, heads=64), "2^18"),
+    (dict(streams=1 << 20, heads=64), "2^18"), (dict(tokens=(1 << 28) + 1), "2^28"),
 ])
 def test_linear_attention_refuses(changes, message):
     a = tokens.linear_attention_args(dtype=0, streams=1, tokens=1, heads=4, kv_heads=2, key_size=8, value_size=8, scale=1.0, q=64, k=64, v=64,
