@@ -2,6 +2,8 @@
 // once and stays on the chip until both outputs are written.
 #include "tokens.h"
 
+#include <algorithm>
+
 namespace cbk {
 namespace {
 
@@ -11,7 +13,7 @@ __device__ __forceinline__ float wave_sum(float v)
     return v;
 }
 
-// Sum over the workgroup of 256; every thread gets it.
+// Sum over a workgroup of 256; every thread gets it.
 __device__ __forceinline__ float block_sum(float v, float *scratch)
 {
     v = wave_sum(v);
@@ -23,20 +25,20 @@ __device__ __forceinline__ float block_sum(float v, float *scratch)
 
 __device__ __forceinline__ float gate_of(float g, int kind)
 {
-    const float open = 1.0f / (1.0f + __expf(-g));
+    const float open = __builtin_amdgcn_rcpf(1.0f + __expf(-g));
     return kind == CBINFER_GATE_SIGMOID ? open : g * open;
 }
 
 // Any size, group, stride and alignment: the row lies in LDS as float32.
 template <int DT, int DS>
-__global__ __launch_bounds__(256) void norm_row_kernel(const cbinfer_gated_norm_args a)
+__global__ __launch_bounds__(256) void norm_row_kernel(const cbinfer_gated_norm_args a, int64_t first)
 {
     typedef typename Elem<DT>::type T;
     typedef typename Elem<DS>::type R;
     extern __shared__ float row[]; // size values, then a factor for each group, then four sums
     const int d = (int)a.size, group = a.group ? a.group : d, groups = d / group, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     float *factor = row + d, *scratch = factor + groups;
-    const int64_t r = blockIdx.x;
+    const int64_t r = first + blockIdx.x;
     const T *x = static_cast<const T *>(a.x) + r * a.x_stride;
     const T *gate = static_cast<const T *>(a.gate) + r * a.gate_stride;
     const R *residual = static_cast<const R *>(a.residual) + r * a.residual_stride;
@@ -71,18 +73,199 @@ __global__ __launch_bounds__(256) void norm_row_kernel(const cbinfer_gated_norm_
     for (int i = threadIdx.x; i < d; i += 256) y[i] = Elem<DT>::put(row[i] * f * a.next_weight[i]);
 }
 
+// Eight values as they lie in memory, 16 bytes at a time.
+template <int DT>
+struct Eight {
+    uint4 u[DT == kF32 ? 2 : 1];
+    __device__ __forceinline__ void load(const typename Elem<DT>::type *p)
+    {
+#pragma unroll
+        for (int i = 0; i < (DT == kF32 ? 2 : 1); ++i) u[i] = reinterpret_cast<const uint4 *>(p)[i];
+    }
+    __device__ __forceinline__ float get(int e) const { return Unit<DT>::get(u[DT == kF32 ? e / 4 : 0], DT == kF32 ? e % 4 : e); }
+    static __device__ __forceinline__ void store(typename Elem<DT>::type *p, const float (&v)[8])
+    {
+        if constexpr (DT == kF32) {
+            reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+            reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        } else {
+            *reinterpret_cast<uint4 *>(p) = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+        }
+    }
+};
+
+// Rows of whole groups of eight values at 16-byte addresses: TPR threads a row, NV times eight values each, in registers from the
+// first load to the last store.  A workgroup goes on to further rows with the weights it has.
+template <int DT, int DS, int TPR, int NV>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(const cbinfer_gated_norm_args a)
+{
+    typedef typename Elem<DT>::type T;
+    typedef typename Elem<DS>::type R;
+    constexpr int ROWS = TPR < 256 ? 256 / TPR : 1, WAVES = TPR / 64;
+    __shared__ float scratch[2][WAVES];
+    extern __shared__ float squares[]; // sums of eight squares, where a group is not a power of two lanes
+    const int d = (int)a.size, thread = threadIdx.x % TPR, lane = threadIdx.x & 63, wave = thread >> 6, eights = d / 8;
+    const int share = a.group ? a.group / 8 : eights; // eights of a group
+    const bool by_lanes = share <= 64 && (share & (share - 1)) == 0, by_row = share == eights;
+    int at[NV];
+    bool there[NV];
+    float w[NV][8], scale[NV][8], next[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        at[i] = (i * TPR + thread) * 8;
+        there[i] = at[i] < d;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            w[i][e] = there[i] && a.weight ? a.weight[at[i] + e] : 1.0f;
+            scale[i][e] = there[i] && a.channel_scale ? a.scale * a.channel_scale[at[i] + e] : a.scale;
+            next[i][e] = there[i] && a.y ? a.next_weight[at[i] + e] : 0.0f;
+        }
+    }
+    auto row_sum = [&](float v, int which) {
+        v = wave_sum(v);
+        if (WAVES > 1) {
+            if (lane == 0) scratch[which][wave] = v;
+            __syncthreads();
+            v = 0.0f;
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) v += scratch[which][i];
+        }
+        return v;
+    };
+    for (int64_t r = (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? threadIdx.x / TPR : 0); r < a.rows; r += (int64_t)gridDim.x * ROWS) {
+        const T *x = static_cast<const T *>(a.x) + r * a.x_stride, *gate = static_cast<const T *>(a.gate) + r * a.gate_stride;
+        const R *residual = static_cast<const R *>(a.residual) + r * a.residual_stride;
+        Eight<DT> xs[NV], gs[NV];
+        Eight<DS> rs[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (there[i]) {
+                xs[i].load(x + at[i]);
+                if (a.gate) gs[i].load(gate + at[i]);
+                if (a.residual) rs[i].load(residual + at[i]);
+            }
+        float u[NV][8], f[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            f[i] = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                u[i][e] = there[i] ? xs[i].get(e) : 0.0f;
+                f[i] = __builtin_fmaf(u[i][e], u[i][e], f[i]);
+            }
+        }
+        if (a.weight) {
+            if (by_row) {
+                float s = 0.0f;
+#pragma unroll
+                for (int i = 0; i < NV; ++i) s += f[i];
+                s = row_sum(s, 0);
+#pragma unroll
+                for (int i = 0; i < NV; ++i) f[i] = s;
+            } else if (by_lanes) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    for (int off = share / 2; off; off >>= 1) f[i] += __shfl_xor(f[i], off);
+            } else {
+                float *mine = squares + (ROWS > 1 ? threadIdx.x / TPR : 0) * eights;
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    if (there[i]) mine[at[i] / 8] = f[i];
+                if (WAVES > 1) __syncthreads(); else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    if (there[i]) {
+                        const int from = at[i] / 8 / share * share;
+                        f[i] = 0.0f;
+                        for (int j = 0; j < share; ++j) f[i] += mine[from + j];
+                    }
+                if (WAVES > 1) __syncthreads(); else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            }
+            const float each = 8 * share;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                f[i] = 1.0f / sqrtf(f[i] / each + a.eps);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[i][e] *= f[i] * w[i][e];
+            }
+        }
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (there[i]) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (a.gate) u[i][e] *= gate_of(gs[i].get(e), a.gate_kind);
+                    u[i][e] = a.residual ? __builtin_fmaf(u[i][e], scale[i][e], rs[i].get(e)) : u[i][e] * scale[i][e];
+                    sum = __builtin_fmaf(u[i][e], u[i][e], sum);
+                }
+                if (a.h) Eight<DS>::store(static_cast<R *>(a.h) + r * a.h_stride + at[i], u[i]);
+            }
+        if (a.y) {
+            sum = row_sum(sum, 1);
+            const float g = 1.0f / sqrtf(sum / d + a.eps);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (there[i]) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) u[i][e] *= g * next[i][e];
+                    Eight<DT>::store(static_cast<T *>(a.y) + r * a.y_stride + at[i], u[i]);
+                }
+        }
+        if (WAVES > 1) __syncthreads(); // the sums are read before the next row's come
+    }
+}
+
+template <int DT, int DS>
+hipError_t by_eights(hipStream_t st, const cbinfer_gated_norm_args &a)
+{
+    const int eights = (int)(a.size / 8);
+    const size_t lds = a.weight && a.group && a.group != a.size ? (size_t)eights * sizeof(float) : 0;
+    // A workgroup reads the weights once for all its rows: few of them pay, if they still cover the memory's latency.  us for 8192
+    // rows of 4096 with a float32 residual and both norms (470 MB) at 256, 512, 768, 1024, 8192 workgroups: 124, 96, 106, 111, 214;
+    // 8192 of 2048 with groups of 128 and a gate alone (101 MB): 42, 26, 23, 22, 34.
+    const int waves = a.y ? 2048 : 4096;
+    auto blocks = [&](int threads, int rows) { return (unsigned)std::min<int64_t>((a.rows + rows - 1) / rows, std::max(256, waves * 64 / threads)); };
+    if (eights <= 64)
+        norm_kernel<DT, DS, 64, 1><<<blocks(256, 4), 256, 4 * lds, st>>>(a);
+    else if (eights <= 256)
+        norm_kernel<DT, DS, 256, 1><<<blocks(256, 1), 256, lds, st>>>(a);
+    else if (eights <= 512)
+        norm_kernel<DT, DS, 256, 2><<<blocks(256, 1), 256, lds, st>>>(a);
+    else if (eights <= 1024)
+        norm_kernel<DT, DS, 512, 2><<<blocks(512, 1), 512, lds, st>>>(a);
+    else
+        norm_kernel<DT, DS, 1024, 2><<<blocks(1024, 1), 1024, lds, st>>>(a);
+    return hipGetLastError();
+}
+
+// Whether every row that is there begins at a 16-byte address.
+bool in_eights(const cbinfer_gated_norm_args &a)
+{
+    const size_t e = a.dtype == kF32 ? 4 : 2, s = a.sum_dtype == kF32 ? 4 : 2;
+    auto fits = [](const void *p, int64_t stride, size_t size) { return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * (int64_t)size % 16 == 0); };
+    return a.size % 8 == 0 && a.group % 8 == 0 && fits(a.x, a.x_stride, e) && fits(a.gate, a.gate_stride, e) && fits(a.y, a.y_stride, e) &&
+           fits(a.residual, a.residual_stride, s) && fits(a.h, a.h_stride, s);
+}
+
+constexpr int64_t kMostBlocks = 1 << 22; // of a launch: threads are counted in 32 bits
+
 } // namespace
 
 hipError_t gated_norm(hipStream_t st, const cbinfer_gated_norm_args &a)
 {
+    if (in_eights(a))
+        return a.dtype == kF32 ? by_eights<kF32, kF32>(st, a) : a.sum_dtype == kF32 ? by_eights<kBF16, kF32>(st, a) : by_eights<kBF16, kBF16>(st, a);
     const int groups = a.group ? (int)(a.size / a.group) : 1;
     const size_t lds = (size_t)(a.size + groups + 4) * sizeof(float);
-    const dim3 grid((unsigned)a.rows);
     auto kernel = a.dtype == kF32 ? norm_row_kernel<kF32, kF32> : a.sum_dtype == kF32 ? norm_row_kernel<kBF16, kF32> : norm_row_kernel<kBF16, kBF16>;
     if (lds > 65536)
         if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return e;
-    kernel<<<grid, 256, lds, st>>>(a);
-    return hipGetLastError();
+    for (int64_t first = 0; first < a.rows; first += kMostBlocks) {
+        kernel<<<(unsigned)std::min(kMostBlocks, a.rows - first), 256, lds, st>>>(a, first);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
 }
 
 } // namespace cbk

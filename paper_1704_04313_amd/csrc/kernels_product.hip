@@ -6,6 +6,9 @@
 // rows][128 / group] bfloat16.  What lies beyond the matrix has code 0 and scale 0.
 #include "tokens.h"
 
+#include <algorithm>
+#include <cstdlib>
+
 namespace cbk {
 namespace {
 
@@ -85,71 +88,250 @@ __global__ __launch_bounds__(256) void quantise_kernel(const typename Elem<DT>::
 }
 
 // ---- the product ---------------------------------------------------------------------------------
-// Eight values of a token from column k on, zeros beyond the row.
+// Eight values of a token from column k on as they lie in memory, zeros beyond the row.
 template <int DT>
-__device__ __forceinline__ void load_eight(const typename Elem<DT>::type *x, int64_t k, int64_t cols, bool there, float (&v)[8])
-{
+struct Eight {
+    uint4 u[DT == kF32 ? 2 : 1];
+    template <bool WHOLE> // rows at 16-byte addresses
+    __device__ __forceinline__ void load(const typename Elem<DT>::type *x, int64_t k, int64_t cols, bool there)
+    {
+        typedef typename Elem<DT>::type T;
+        constexpr int N = DT == kF32 ? 2 : 1;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = there && k + e < cols ? Elem<DT>::get(x[k + e]) : 0.0f;
-}
+        for (int i = 0; i < N; ++i) u[i] = make_uint4(0, 0, 0, 0);
+        if (!there || k >= cols) return;
+        if (WHOLE && k + 8 <= cols) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) u[i] = reinterpret_cast<const uint4 *>(x + k)[i];
+            return;
+        }
+        union { T e[8]; uint4 u[N]; } v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v.e[e] = k + e < cols ? x[k + e] : T(0);
+#pragma unroll
+        for (int i = 0; i < N; ++i) u[i] = v.u[i];
+    }
+    __device__ __forceinline__ float get(int e) const { return Unit<DT>::get(u[DT == kF32 ? e / 4 : 0], DT == kF32 ? e % 4 : e); }
+};
 
 // A float as the sum of three bfloat16, exactly: eight bits are cut off each time.  Infinities stay in the first.
-template <int PARTS>
-__device__ __forceinline__ void split(const float (&v)[8], bf16x8 (&p)[PARTS])
+__device__ __forceinline__ void parts_of(const Eight<kBF16> &v, bf16x8 (&p)[1]) { p[0] = __builtin_bit_cast(bf16x8, v.u[0]); }
+__device__ __forceinline__ void parts_of(const Eight<kF32> &v, bf16x8 (&p)[3])
 {
+    constexpr int PARTS = 3;
+    float r[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        float r = v[e];
+    for (int e = 0; e < 8; ++e) r[e] = v.get(e);
 #pragma unroll
-        for (int i = 0; i < PARTS; ++i) {
-            const float top = __uint_as_float(__float_as_uint(r) & 0xffff0000u);
-            p[i][e] = (__bf16)top;
-            r = __builtin_isinf(top) ? 0.0f : r - top;
-        }
+    for (int i = 0; i < PARTS; ++i) {
+        uint4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) (&w.x)[j] = __builtin_amdgcn_perm(__float_as_uint(r[2 * j + 1]), __float_as_uint(r[2 * j]), 0x07060302u);
+        p[i] = __builtin_bit_cast(bf16x8, w);
+        if (i + 1 < PARTS)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float top = __uint_as_float(__float_as_uint(r[e]) & 0xffff0000u);
+                r[e] = __builtin_isinf(top) ? 0.0f : r[e] - top;
+            }
     }
 }
 
-// A workgroup multiplies one tile of 16 rows with 16 tokens; its four waves take the blocks of columns in turn.
-template <int DT>
-__global__ __launch_bounds__(256) void product_kernel(const cbinfer_quantised_product_args a, const uint16_t *scales, int blocks)
+// A wave multiplies R tiles of 16 rows with MT tiles of 16 tokens over its share of the blocks of columns: the waves of a
+// workgroup take them in turn and add up through LDS.  blockIdx.y: a part of the blocks (their sums then go to `partial`, part by part),
+// blockIdx.z: the tokens.  Tokens are the matrix instruction's rows, weights its columns: a lane has one row's scale at a time.
+template <int DT, int MT, int R, bool WHOLE>
+__global__ __launch_bounds__(512) void product_kernel(const cbinfer_quantised_product_args a, const uint16_t *scales, int blocks, int tiles, int per, float *partial)
 {
     typedef typename Elem<DT>::type T;
     constexpr int PARTS = DT == kF32 ? 3 : 1;
-    __shared__ float sums[4][256];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per_block = 128 / a.group;
-    const int64_t tile = blockIdx.x, token = (int64_t)blockIdx.y * 16 + (lane & 15);
-    const uint4 *codes = static_cast<const uint4 *>(a.packed) + tile * blocks * 64 + lane;
-    const uint16_t *sc = scales + (tile * blocks * 16 + (lane & 15)) * per_block;
-    const T *x = static_cast<const T *>(a.x) + token * a.x_stride;
-    const bool there = token < a.tokens;
-    f32x4 acc = {0, 0, 0, 0};
-    for (int b = wave; b < blocks; b += 4) {
-        const uint4 w = codes[(int64_t)b * 64];
-        f32x4 part = {0, 0, 0, 0};
+    extern __shared__ f32x4 sums[]; // [wave][R][MT][lane]
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, per_block = 128 / a.group, step = a.group / 32;
+    const int64_t token0 = (int64_t)blockIdx.z * (16 * MT), tile0 = (int64_t)blockIdx.x * R;
+    const T *x[MT];
+    bool there[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int64_t t = token0 + 16 * i + (lane & 15);
+        there[i] = t < a.tokens;
+        x[i] = static_cast<const T *>(a.x) + (there[i] ? t : 0) * a.x_stride;
+    }
+    const uint4 *codes[R];
+    const uint16_t *sc[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int64_t tile = tile0 + r < tiles ? tile0 + r : tiles - 1; // beyond the last: computed again, not written
+        codes[r] = static_cast<const uint4 *>(a.packed) + tile * blocks * 64 + lane;
+        sc[r] = scales + (tile * blocks * 16 + (lane & 15)) * per_block;
+    }
+    f32x4 acc[R][MT];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) acc[r][i] = f32x4{0, 0, 0, 0};
+    const int end = min(blocks, ((int)blockIdx.y + 1) * per);
+    // of a block: the codes, the scales of a row, and with one tile of tokens their values;
+    // the next block's are on their way while one is worked on
+    struct Block {
+        uint4 w[R];
+        uint2 s[R];
+        Eight<DT> x[4];
+    };
+    auto values = [&](int b, int j, int i) {
+        Eight<DT> v;
+        v.template load<WHOLE>(x[i], (int64_t)b * 128 + j * 32 + (lane >> 4) * 8, a.cols, there[i]);
+        return v;
+    };
+    auto load = [&](Block &k, int b) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            k.w[r] = codes[r][(int64_t)b * 64];
+            const uint16_t *p = sc[r] + (int64_t)b * 16 * per_block;
+            if (step == 1)
+                k.s[r] = *reinterpret_cast<const uint2 *>(p);
+            else if (step == 2)
+                k.s[r].x = *reinterpret_cast<const unsigned *>(p);
+            else
+                k.s[r].x = *p;
+        }
+        if (MT == 1)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) k.x[j] = values(b, j, 0);
+    };
+    Block next;
+    int b = blockIdx.y * per + wave;
+    if (b < end) load(next, b);
+    for (; b < end; b += waves) {
+        const Block now = next;
+        if (b + waves < end) load(next, b + waves);
+        f32x4 part[R][MT];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            float v[8];
-            bf16x8 p[PARTS];
-            load_eight<DT>(x, (int64_t)b * 128 + j * 32 + (lane >> 4) * 8, a.cols, there, v);
-            split<PARTS>(v, p);
-            const bf16x8 q = values_of((&w.x)[j]);
+            if (j % step == 0)
 #pragma unroll
-            for (int i = 0; i < PARTS; ++i) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[i], q, part, 0, 0, 0);
-            if ((j + 1) * 32 % a.group == 0) { // the group ends here
-                const float s = Elem<kBF16>::get(sc[(int64_t)b * 16 * per_block + j * 32 / a.group]);
+                for (int r = 0; r < R; ++r)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) acc[r] = __builtin_fmaf(s, part[r], acc[r]);
-                part = {0, 0, 0, 0};
+                    for (int i = 0; i < MT; ++i) part[r][i] = f32x4{0, 0, 0, 0};
+            bf16x8 p[MT][PARTS];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                parts_of(MT == 1 ? now.x[j] : values(b, j, i), p[i]);
             }
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const bf16x8 q = values_of((&now.w[r].x)[j]);
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int k = 0; k < PARTS; ++k) part[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[i][k], q, part[r][i], 0, 0, 0);
+            }
+            if ((j + 1) % step == 0) // the group ends here
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const int g = step == 1 ? j : step == 2 ? j / 2 : 0; // of the block's groups
+                    const unsigned u = g < 2 ? now.s[r].x : now.s[r].y;
+                    const float s = __uint_as_float(g & 1 ? u & 0xffff0000u : u << 16);
+#pragma unroll
+                    for (int i = 0; i < MT; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[r][i][e] = __builtin_fmaf(s, part[r][i][e], acc[r][i][e]);
+                }
         }
     }
+    if (waves > 1) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) sums[wave][r * 64 + lane] = acc[r];
-    __syncthreads();
-    const int i = threadIdx.x, n16 = i & 15, t16 = ((i & 63) >> 4) * 4 + (i >> 6);
-    const int64_t n = tile * 16 + n16, t = (int64_t)blockIdx.y * 16 + t16;
-    if (n < a.rows && t < a.tokens)
-        static_cast<T *>(a.y)[t * a.y_stride + n] = Elem<DT>::put((sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]) + (a.bias ? a.bias[n] : 0.0f));
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < MT; ++i) sums[(wave * R * MT + r * MT + i) * 64 + lane] = acc[r][i];
+        __syncthreads();
+    }
+    // a wave writes tiles of its own
+    for (int at = wave; at < R * MT; at += waves) {
+        const int r = at / MT, i = at - r * MT;
+        f32x4 y = {0, 0, 0, 0};
+        if (waves > 1) {
+            for (int k = 0; k < waves; ++k) y += sums[(k * R * MT + at) * 64 + lane];
+        } else {
+#pragma unroll
+            for (int k = 0; k < R * MT; ++k)
+                if (k == at) y = acc[k / MT][k % MT];
+        }
+        const int64_t n = (tile0 + r) * 16 + (lane & 15), t = token0 + 16 * i + (lane >> 4) * 4;
+        if (tile0 + r >= tiles || n >= a.rows) continue;
+        const float bias = a.bias && !partial ? a.bias[n] : 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (t + e < a.tokens) {
+                if (partial)
+                    partial[((int64_t)blockIdx.y * a.tokens + t + e) * a.rows + n] = y[e];
+                else
+                    static_cast<T *>(a.y)[(t + e) * a.y_stride + n] = Elem<DT>::put(y[e] + bias);
+            }
+    }
+}
+
+// The parts' sums, in order.
+template <int DT>
+__global__ __launch_bounds__(256) void join_parts_kernel(const cbinfer_quantised_product_args a, int parts, const float *partial)
+{
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, all = a.tokens * a.rows;
+    if (at >= all) return;
+    const int64_t t = at / a.rows, n = at - t * a.rows;
+    float y = a.bias ? a.bias[n] : 0.0f;
+    for (int p = 0; p < parts; ++p) y += partial[p * all + at];
+    static_cast<typename Elem<DT>::type *>(a.y)[t * a.y_stride + n] = Elem<DT>::put(y);
+}
+
+struct Plan {
+    int mt, r, waves, parts, per;
+};
+
+Plan plan(const cbinfer_quantised_product_args &a)
+{
+    Plan p;
+    const int64_t tiles = tiles_of(a.rows), blocks = blocks_of(a.cols);
+    p.mt = a.tokens <= 16 ? 1 : a.tokens <= 32 ? 2 : 4;
+    static const int R_ = getenv("CBR") ? atoi(getenv("CBR")) : 0, W_ = getenv("CBW") ? atoi(getenv("CBW")) : 0, P_ = getenv("CBP") ? atoi(getenv("CBP")) : 0;
+    p.r = R_ ? R_ : tiles >= 2048 ? 4 : tiles >= 512 ? 2 : 1;
+    p.waves = W_ ? W_ : 8;
+    while (p.waves * p.r * p.mt > 64) p.waves /= 2; // their sums in 64 KiB of LDS
+    p.parts = P_ ? P_ : 1;
+    p.per = (int)((blocks + p.parts - 1) / p.parts);
+    p.parts = (int)((blocks + p.per - 1) / p.per);
+    return p;
+}
+
+template <int DT, int MT, int R>
+hipError_t launch(hipStream_t st, const cbinfer_quantised_product_args &a, const Plan &p)
+{
+    const int64_t tiles = tiles_of(a.rows), blocks = blocks_of(a.cols);
+    const uint16_t *scales = reinterpret_cast<const uint16_t *>(static_cast<const char *>(a.packed) + code_bytes(a.rows, a.cols));
+    const bool whole = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.x_stride * (DT == kF32 ? 4 : 2) % 16 == 0;
+    float *partial = p.parts > 1 ? static_cast<float *>(a.workspace) : nullptr;
+    const dim3 grid((unsigned)((tiles + R - 1) / R), p.parts, (unsigned)((a.tokens + 16 * MT - 1) / (16 * MT)));
+    const size_t lds = p.waves > 1 ? (size_t)p.waves * R * MT * 64 * sizeof(f32x4) : 0;
+    if (whole)
+        product_kernel<DT, MT, R, true><<<grid, p.waves * 64, lds, st>>>(a, scales, (int)blocks, (int)tiles, p.per, partial);
+    else
+        product_kernel<DT, MT, R, false><<<grid, p.waves * 64, lds, st>>>(a, scales, (int)blocks, (int)tiles, p.per, partial);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (partial) {
+        join_parts_kernel<DT><<<(unsigned)((a.tokens * a.rows + 255) / 256), 256, 0, st>>>(a, p.parts, partial);
+        return hipGetLastError();
+    }
+    return hipSuccess;
+}
+
+template <int DT, int MT>
+hipError_t launch_rows(hipStream_t st, const cbinfer_quantised_product_args &a, const Plan &p)
+{
+    return p.r == 4 ? launch<DT, MT, 4>(st, a, p) : p.r == 2 ? launch<DT, MT, 2>(st, a, p) : launch<DT, MT, 1>(st, a, p);
+}
+
+template <int DT>
+hipError_t launch_any(hipStream_t st, const cbinfer_quantised_product_args &a, const Plan &p)
+{
+    return p.mt == 1 ? launch_rows<DT, 1>(st, a, p) : p.mt == 2 ? launch_rows<DT, 2>(st, a, p) : launch_rows<DT, 4>(st, a, p);
 }
 
 } // namespace
@@ -182,17 +364,16 @@ hipError_t pack_weights(hipStream_t st, const uint8_t *codes, const uint16_t *sc
     return hipGetLastError();
 }
 
-size_t quantised_product_workspace(const cbinfer_quantised_product_args &) { return 0; }
+size_t quantised_product_workspace(const cbinfer_quantised_product_args &a)
+{
+    const Plan p = plan(a);
+    return p.parts > 1 ? (size_t)p.parts * a.tokens * a.rows * sizeof(float) : 0;
+}
 
 hipError_t quantised_product(hipStream_t st, const cbinfer_quantised_product_args &a)
 {
-    const dim3 grid((unsigned)tiles_of(a.rows), (unsigned)((a.tokens + 15) / 16));
-    const uint16_t *scales = reinterpret_cast<const uint16_t *>(static_cast<const char *>(a.packed) + code_bytes(a.rows, a.cols));
-    if (a.dtype == kF32)
-        product_kernel<kF32><<<grid, 256, 0, st>>>(a, scales, (int)blocks_of(a.cols));
-    else
-        product_kernel<kBF16><<<grid, 256, 0, st>>>(a, scales, (int)blocks_of(a.cols));
-    return hipGetLastError();
+    const Plan p = plan(a);
+    return a.dtype == kF32 ? launch_any<kF32>(st, a, p) : launch_any<kBF16>(st, a, p);
 }
 
 } // namespace cbk
