@@ -7,7 +7,6 @@
 #include "tokens.h"
 
 #include <algorithm>
-#include <cstdlib>
 
 namespace cbk {
 namespace {
@@ -91,23 +90,23 @@ __global__ __launch_bounds__(256) void quantise_kernel(const typename Elem<DT>::
 // Eight values of a token from column k on as they lie in memory, zeros beyond the row.
 template <int DT>
 struct Eight {
-    uint4 u[DT == kF32 ? 2 : 1];
-    template <bool WHOLE> // rows at 16-byte addresses
-    __device__ __forceinline__ void load(const typename Elem<DT>::type *x, int64_t k, int64_t cols, bool there)
+    static constexpr int N = DT == kF32 ? 2 : 1;
+    uint4 u[N];
+    // at a 16-byte address; the address is valid also where the token is not there
+    __device__ __forceinline__ void load(const typename Elem<DT>::type *x, bool there)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            u[i] = reinterpret_cast<const uint4 *>(x)[i];
+            if (!there) u[i] = make_uint4(0, 0, 0, 0);
+        }
+    }
+    __device__ __forceinline__ void load_singly(const typename Elem<DT>::type *x, int64_t k, int64_t cols, bool there)
     {
         typedef typename Elem<DT>::type T;
-        constexpr int N = DT == kF32 ? 2 : 1;
-#pragma unroll
-        for (int i = 0; i < N; ++i) u[i] = make_uint4(0, 0, 0, 0);
-        if (!there || k >= cols) return;
-        if (WHOLE && k + 8 <= cols) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) u[i] = reinterpret_cast<const uint4 *>(x + k)[i];
-            return;
-        }
         union { T e[8]; uint4 u[N]; } v;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v.e[e] = k + e < cols ? x[k + e] : T(0);
+        for (int e = 0; e < 8; ++e) v.e[e] = there && k + e < cols ? x[k + e] : T(0);
 #pragma unroll
         for (int i = 0; i < N; ++i) u[i] = v.u[i];
     }
@@ -137,201 +136,210 @@ __device__ __forceinline__ void parts_of(const Eight<kF32> &v, bf16x8 (&p)[3])
     }
 }
 
-// A wave multiplies R tiles of 16 rows with MT tiles of 16 tokens over its share of the blocks of columns: the waves of a
-// workgroup take them in turn and add up through LDS.  blockIdx.y: a part of the blocks (their sums then go to `partial`, part by part),
-// blockIdx.z: the tokens.  Tokens are the matrix instruction's rows, weights its columns: a lane has one row's scale at a time.
-template <int DT, int MT, int R, bool WHOLE>
-__global__ __launch_bounds__(512) void product_kernel(const cbinfer_quantised_product_args a, const uint16_t *scales, int blocks, int tiles, int per, float *partial)
+// A workgroup keeps its part of the columns of MT tiles of 16 tokens in registers, each of its waves BP blocks of them, and
+// streams weights past them: R tiles of 16 rows at a time, the next on their way while these are multiplied.  The waves add up
+// through LDS.  blockIdx.y: the part of the columns (of several, each leaves its sums in `partial`), blockIdx.z: the tokens.
+// Tokens are the matrix instruction's rows, weights its columns, so that a lane needs one row's scales.
+template <int DT, int MT, int BP, int R, int WAVES, int PER_CU>
+__global__ __launch_bounds__(WAVES * 64, WAVES * PER_CU / 4) void product_kernel(const cbinfer_quantised_product_args a, const uint16_t *scales, int blocks, int tiles, int whole, float *partial)
 {
     typedef typename Elem<DT>::type T;
     constexpr int PARTS = DT == kF32 ? 3 : 1;
-    extern __shared__ f32x4 sums[]; // [wave][R][MT][lane]
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, per_block = 128 / a.group, step = a.group / 32;
-    const int64_t token0 = (int64_t)blockIdx.z * (16 * MT), tile0 = (int64_t)blockIdx.x * R;
-    const T *x[MT];
-    bool there[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const int64_t t = token0 + 16 * i + (lane & 15);
-        there[i] = t < a.tokens;
-        x[i] = static_cast<const T *>(a.x) + (there[i] ? t : 0) * a.x_stride;
-    }
-    const uint4 *codes[R];
-    const uint16_t *sc[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int64_t tile = tile0 + r < tiles ? tile0 + r : tiles - 1; // beyond the last: computed again, not written
-        codes[r] = static_cast<const uint4 *>(a.packed) + tile * blocks * 64 + lane;
-        sc[r] = scales + (tile * blocks * 16 + (lane & 15)) * per_block;
-    }
-    f32x4 acc[R][MT];
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int i = 0; i < MT; ++i) acc[r][i] = f32x4{0, 0, 0, 0};
-    const int end = min(blocks, ((int)blockIdx.y + 1) * per);
-    // of a block: the codes, the scales of a row, and with one tile of tokens their values;
-    // the next block's are on their way while one is worked on
-    struct Block {
-        uint4 w[R];
-        uint2 s[R];
-        Eight<DT> x[4];
+    __shared__ f32x4 sums[2][WAVES][R * MT][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per_block = 128 / a.group, step = a.group / 32;
+    const int64_t token0 = (int64_t)blockIdx.z * (16 * MT);
+    const int block0 = blockIdx.y * (WAVES * BP) + wave; // then every WAVES-th
+
+    struct Weights {
+        uint4 w[R][BP];
+        uint2 s[R][BP];
     };
-    auto values = [&](int b, int j, int i) {
-        Eight<DT> v;
-        v.template load<WHOLE>(x[i], (int64_t)b * 128 + j * 32 + (lane >> 4) * 8, a.cols, there[i]);
-        return v;
+    const uint4 *codes = static_cast<const uint4 *>(a.packed) + lane;
+    const uint16_t *sc = scales + (lane & 15) * per_block;
+    Weights k; // each of its blocks is read again, for the next turn, as soon as it has been multiplied
+    auto load = [&](int group, int r, int i) {
+        const int64_t tile = min(group * R + r, tiles - 1); // beyond the last: multiplied again, not written
+        const int64_t at = tile * blocks + min(block0 + i * WAVES, blocks - 1); // beyond the last: times zeros
+        k.w[r][i] = codes[at * 64];
+        const uint16_t *p = sc + at * 16 * per_block;
+        if (step == 1)
+            k.s[r][i] = *reinterpret_cast<const uint2 *>(p);
+        else if (step == 2)
+            k.s[r][i].x = *reinterpret_cast<const unsigned *>(p);
+        else
+            k.s[r][i].x = *p;
     };
-    auto load = [&](Block &k, int b) {
+    const int groups = (tiles + R - 1) / R;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            k.w[r] = codes[r][(int64_t)b * 64];
-            const uint16_t *p = sc[r] + (int64_t)b * 16 * per_block;
-            if (step == 1)
-                k.s[r] = *reinterpret_cast<const uint2 *>(p);
-            else if (step == 2)
-                k.s[r].x = *reinterpret_cast<const unsigned *>(p);
-            else
-                k.s[r].x = *p;
-        }
-        if (MT == 1)
+    for (int i = 0; i < BP; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) k.x[j] = values(b, j, 0);
-    };
-    Block next;
-    int b = blockIdx.y * per + wave;
-    if (b < end) load(next, b);
-    for (; b < end; b += waves) {
-        const Block now = next;
-        if (b + waves < end) load(next, b + waves);
-        f32x4 part[R][MT];
+        for (int r = 0; r < R; ++r) load(blockIdx.x, r, i);
+
+    bf16x8 x[MT][BP][4][PARTS];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (j % step == 0)
+    for (int m = 0; m < MT; ++m) {
+        const int64_t t = token0 + 16 * m + (lane & 15);
+        const T *row = static_cast<const T *>(a.x) + (t < a.tokens ? t : 0) * a.x_stride;
 #pragma unroll
-                for (int r = 0; r < R; ++r)
+        for (int i = 0; i < BP; ++i) {
+            const int64_t k0 = (int64_t)(block0 + i * WAVES) * 128;
+            Eight<DT> v[4];
+            if (whole && k0 + 128 <= a.cols) {
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) part[r][i] = f32x4{0, 0, 0, 0};
-            bf16x8 p[MT][PARTS];
+                for (int j = 0; j < 4; ++j) v[j].load(row + k0 + j * 32 + (lane >> 4) * 8, t < a.tokens);
+            } else {
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                parts_of(MT == 1 ? now.x[j] : values(b, j, i), p[i]);
-            }
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const bf16x8 q = values_of((&now.w[r].x)[j]);
-#pragma unroll
-                for (int i = 0; i < MT; ++i)
-#pragma unroll
-                    for (int k = 0; k < PARTS; ++k) part[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[i][k], q, part[r][i], 0, 0, 0);
-            }
-            if ((j + 1) % step == 0) // the group ends here
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const int g = step == 1 ? j : step == 2 ? j / 2 : 0; // of the block's groups
-                    const unsigned u = g < 2 ? now.s[r].x : now.s[r].y;
-                    const float s = __uint_as_float(g & 1 ? u & 0xffff0000u : u << 16);
-#pragma unroll
-                    for (int i = 0; i < MT; ++i)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[r][i][e] = __builtin_fmaf(s, part[r][i][e], acc[r][i][e]);
+                for (int j = 0; j < 4; ++j) {
+                    v[j].load_singly(row, k0 + j * 32 + (lane >> 4) * 8, a.cols, t < a.tokens);
+                    asm volatile("" ::: "memory"); // one after the other: together they would take most of the registers
                 }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) parts_of(v[j], x[m][i][j]);
         }
     }
-    if (waves > 1) {
+
+    int turn = 0;
+    for (int group = blockIdx.x; group < groups; group += gridDim.x, turn ^= 1) {
+        const int then = min(group + (int)gridDim.x, groups - 1);
+        f32x4 acc[R][MT];
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int i = 0; i < MT; ++i) sums[(wave * R * MT + r * MT + i) * 64 + lane] = acc[r][i];
-        __syncthreads();
-    }
-    // a wave writes tiles of its own
-    for (int at = wave; at < R * MT; at += waves) {
-        const int r = at / MT, i = at - r * MT;
-        f32x4 y = {0, 0, 0, 0};
-        if (waves > 1) {
-            for (int k = 0; k < waves; ++k) y += sums[(k * R * MT + at) * 64 + lane];
-        } else {
+            for (int m = 0; m < MT; ++m) acc[r][m] = f32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int k = 0; k < R * MT; ++k)
-                if (k == at) y = acc[k / MT][k % MT];
-        }
-        const int64_t n = (tile0 + r) * 16 + (lane & 15), t = token0 + 16 * i + (lane >> 4) * 4;
-        if (tile0 + r >= tiles || n >= a.rows) continue;
-        const float bias = a.bias && !partial ? a.bias[n] : 0.0f;
+        for (int i = 0; i < BP; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (t + e < a.tokens) {
-                if (partial)
-                    partial[((int64_t)blockIdx.y * a.tokens + t + e) * a.rows + n] = y[e];
-                else
-                    static_cast<T *>(a.y)[(t + e) * a.y_stride + n] = Elem<DT>::put(y[e] + bias);
+            for (int r = 0; r < R; ++r) {
+                const uint4 w = k.w[r][i];
+                const uint2 s2 = k.s[r][i];
+                f32x4 part[MT];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (j % step == 0)
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) part[m] = f32x4{0, 0, 0, 0};
+                    const bf16x8 q = values_of((&w.x)[j]);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int p = 0; p < PARTS; ++p) part[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[m][i][j][p], q, part[m], 0, 0, 0);
+                    if ((j + 1) % step == 0) { // the group ends here
+                        const int g = step == 1 ? j : step == 2 ? j / 2 : 0; // of the block's groups
+                        const unsigned u = g < 2 ? s2.x : s2.y;
+                        const float s = __uint_as_float(g & 1 ? u & 0xffff0000u : u << 16);
+#pragma unroll
+                        for (int m = 0; m < MT; ++m)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[r][m][e] = __builtin_fmaf(s, part[m][e], acc[r][m][e]);
+                    }
+                }
+                load(then, r, i);
             }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) sums[turn][wave][r * MT + m][lane] = acc[r][m];
+        __syncthreads(); // the other turn's sums were read before this
+        for (int at = wave; at < R * MT; at += WAVES) {
+            f32x4 y = sums[turn][0][at][lane];
+#pragma unroll 4 // more at a time would cost registers that hold x
+            for (int w = 1; w < WAVES; ++w) {
+                const f32x4 z = sums[turn][w][at][lane];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] += z[e];
+            }
+            const int r = at / MT, m = at - r * MT;
+            const int64_t n = ((int64_t)group * R + r) * 16 + (lane & 15), t = token0 + 16 * m + (lane >> 4) * 4;
+            if (n >= a.rows) continue;
+            const float bias = a.bias && !partial ? a.bias[n] : 0.0f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (t + e < a.tokens) {
+                    if (partial)
+                        partial[((int64_t)blockIdx.y * a.tokens + t + e) * a.rows + n] = y[e];
+                    else
+                        static_cast<T *>(a.y)[(t + e) * a.y_stride + n] = Elem<DT>::put(y[e] + bias);
+                }
+        }
     }
 }
 
-// The parts' sums, in order.
+// The parts' sums, in order; blockIdx.y: the token.
 template <int DT>
 __global__ __launch_bounds__(256) void join_parts_kernel(const cbinfer_quantised_product_args a, int parts, const float *partial)
 {
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, all = a.tokens * a.rows;
-    if (at >= all) return;
-    const int64_t t = at / a.rows, n = at - t * a.rows;
-    float y = a.bias ? a.bias[n] : 0.0f;
-    for (int p = 0; p < parts; ++p) y += partial[p * all + at];
-    static_cast<typename Elem<DT>::type *>(a.y)[t * a.y_stride + n] = Elem<DT>::put(y);
+    const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x, step = a.tokens * a.rows;
+    if (n >= a.rows) return;
+    for (int64_t t = blockIdx.y; t < a.tokens; t += gridDim.y) {
+        const float *p = partial + t * a.rows + n;
+        float y = a.bias ? a.bias[n] : 0.0f;
+        int i = 0;
+        for (; i + 8 <= parts; i += 8) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = p[(i + k) * step];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) y += v[k];
+        }
+        for (; i < parts; ++i) y += p[i * step];
+        static_cast<typename Elem<DT>::type *>(a.y)[t * a.y_stride + n] = Elem<DT>::put(y);
+    }
 }
 
-struct Plan {
-    int mt, r, waves, parts, per;
+// PER_CU: workgroups that run on a compute unit at a time.
+template <int DT, int MT, int BP, int R, int WAVES, int PER_CU>
+struct Shape {
+    static int parts(const cbinfer_quantised_product_args &a) { return (int)((blocks_of(a.cols) + WAVES * BP - 1) / (WAVES * BP)); }
+    static hipError_t run(hipStream_t st, const cbinfer_quantised_product_args &a)
+    {
+        const int64_t tiles = tiles_of(a.rows), blocks = blocks_of(a.cols), groups = (tiles + R - 1) / R;
+        const uint16_t *scales = reinterpret_cast<const uint16_t *>(static_cast<const char *>(a.packed) + code_bytes(a.rows, a.cols));
+        const int whole = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.x_stride * (DT == kF32 ? 4 : 2) % 16 == 0, n = parts(a);
+        float *partial = n > 1 ? static_cast<float *>(a.workspace) : nullptr;
+        const unsigned z = (unsigned)((a.tokens + 16 * MT - 1) / (16 * MT));
+        // as many workgroups as run at a time, each with the same number of turns or one less
+        const int64_t room = std::max<int64_t>(1, 256 * PER_CU / (n * z)), turns = (groups + room - 1) / room;
+        const dim3 grid((unsigned)((groups + turns - 1) / turns), n, z);
+        product_kernel<DT, MT, BP, R, WAVES, PER_CU><<<grid, WAVES * 64, 0, st>>>(a, scales, (int)blocks, (int)tiles, whole, partial);
+        if (hipError_t e = hipGetLastError()) return e;
+        if (partial) {
+            join_parts_kernel<DT><<<dim3((unsigned)((a.rows + 255) / 256), (unsigned)std::min<int64_t>(a.tokens, 1024)), 256, 0, st>>>(a, n, partial);
+            return hipGetLastError();
+        }
+        return hipSuccess;
+    }
 };
 
-Plan plan(const cbinfer_quantised_product_args &a)
-{
-    Plan p;
-    const int64_t tiles = tiles_of(a.rows), blocks = blocks_of(a.cols);
-    p.mt = a.tokens <= 16 ? 1 : a.tokens <= 32 ? 2 : 4;
-    static const int R_ = getenv("CBR") ? atoi(getenv("CBR")) : 0, W_ = getenv("CBW") ? atoi(getenv("CBW")) : 0, P_ = getenv("CBP") ? atoi(getenv("CBP")) : 0;
-    p.r = R_ ? R_ : tiles >= 2048 ? 4 : tiles >= 512 ? 2 : 1;
-    p.waves = W_ ? W_ : 8;
-    while (p.waves * p.r * p.mt > 64) p.waves /= 2; // their sums in 64 KiB of LDS
-    p.parts = P_ ? P_ : 1;
-    p.per = (int)((blocks + p.parts - 1) / p.parts);
-    p.parts = (int)((blocks + p.per - 1) / p.per);
-    return p;
-}
-
-template <int DT, int MT, int R>
-hipError_t launch(hipStream_t st, const cbinfer_quantised_product_args &a, const Plan &p)
+// Calls f with the shape for these sizes.  A workgroup's waves times their blocks should be the blocks of a row, or a part of
+// them without much left over: waves without a block wait for the others.
+template <int DT, typename F>
+auto with_shape(const cbinfer_quantised_product_args &a, F f)
 {
     const int64_t tiles = tiles_of(a.rows), blocks = blocks_of(a.cols);
-    const uint16_t *scales = reinterpret_cast<const uint16_t *>(static_cast<const char *>(a.packed) + code_bytes(a.rows, a.cols));
-    const bool whole = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.x_stride * (DT == kF32 ? 4 : 2) % 16 == 0;
-    float *partial = p.parts > 1 ? static_cast<float *>(a.workspace) : nullptr;
-    const dim3 grid((unsigned)((tiles + R - 1) / R), p.parts, (unsigned)((a.tokens + 16 * MT - 1) / (16 * MT)));
-    const size_t lds = p.waves > 1 ? (size_t)p.waves * R * MT * 64 * sizeof(f32x4) : 0;
-    if (whole)
-        product_kernel<DT, MT, R, true><<<grid, p.waves * 64, lds, st>>>(a, scales, (int)blocks, (int)tiles, p.per, partial);
-    else
-        product_kernel<DT, MT, R, false><<<grid, p.waves * 64, lds, st>>>(a, scales, (int)blocks, (int)tiles, p.per, partial);
-    if (hipError_t e = hipGetLastError()) return e;
-    if (partial) {
-        join_parts_kernel<DT><<<(unsigned)((a.tokens * a.rows + 255) / 256), 256, 0, st>>>(a, p.parts, partial);
-        return hipGetLastError();
+    if constexpr (DT == kBF16) {
+        if (a.tokens <= 16) {
+            if (blocks <= 8) return f(Shape<DT, 1, 1, 4, 8, 2>());
+            // us for 100003 x 2048 (115 MB) and 16 tokens: R = 3 33.5, 2 36.0, 4 (registers spill) 35.7; 16 waves, half of them without a block, 55
+            if (blocks <= 16) return f(Shape<DT, 1, 2, 3, 8, 2>());
+            if (blocks <= 32) {
+                // one token, 4096 x 4096: a row's tiles one by one 9.2, in two parts of 8 waves 14
+                if (tiles <= 512) return f(Shape<DT, 1, 2, 1, 16, 1>());
+                // 16 tokens, 100003 x 4096: 48.8, in two parts 50.3
+                return f(Shape<DT, 1, 2, 2, 16, 1>());
+            }
+            // 4 tokens, 4729 x 20806: parts of 16 blocks 26.8, of 32 27.3
+            return f(Shape<DT, 1, 2, 2, 8, 2>());
+        }
+        // 64 tokens, 100003 x 2048: four tiles of tokens at a time 62, two (the weights pass twice) 97; 4096 x 4096: 17.6, 15.3
+        if (a.tokens > 32 && tiles >= 1024) return f(Shape<DT, 4, 2, 2, 8, 1>());
+        return f(Shape<DT, 2, 2, 2, 8, 1>());
+    } else {
+        // three parts of x take three times the registers.  16 tokens, 36122 x 5669: 48.9, with 16 waves 50.8
+        if (a.tokens <= 16) return f(Shape<DT, 1, 1, 4, 8, 2>());
+        // 64 tokens, 256 x 38400: two tiles at a time 20.8, four 29; 8192 x 2048: 20.8, 28.6
+        return f(Shape<DT, 2, 1, 2, 8, 1>());
     }
-    return hipSuccess;
-}
-
-template <int DT, int MT>
-hipError_t launch_rows(hipStream_t st, const cbinfer_quantised_product_args &a, const Plan &p)
-{
-    return p.r == 4 ? launch<DT, MT, 4>(st, a, p) : p.r == 2 ? launch<DT, MT, 2>(st, a, p) : launch<DT, MT, 1>(st, a, p);
-}
-
-template <int DT>
-hipError_t launch_any(hipStream_t st, const cbinfer_quantised_product_args &a, const Plan &p)
-{
-    return p.mt == 1 ? launch_rows<DT, 1>(st, a, p) : p.mt == 2 ? launch_rows<DT, 2>(st, a, p) : launch_rows<DT, 4>(st, a, p);
 }
 
 } // namespace
@@ -366,14 +374,15 @@ hipError_t pack_weights(hipStream_t st, const uint8_t *codes, const uint16_t *sc
 
 size_t quantised_product_workspace(const cbinfer_quantised_product_args &a)
 {
-    const Plan p = plan(a);
-    return p.parts > 1 ? (size_t)p.parts * a.tokens * a.rows * sizeof(float) : 0;
+    const auto parts = [&](auto shape) { return shape.parts(a); };
+    const int n = a.dtype == kF32 ? with_shape<kF32>(a, parts) : with_shape<kBF16>(a, parts);
+    return n > 1 ? (size_t)n * a.tokens * a.rows * sizeof(float) : 0;
 }
 
 hipError_t quantised_product(hipStream_t st, const cbinfer_quantised_product_args &a)
 {
-    const Plan p = plan(a);
-    return a.dtype == kF32 ? launch_any<kF32>(st, a, p) : launch_any<kBF16>(st, a, p);
+    const auto run = [&](auto shape) { return shape.run(st, a); };
+    return a.dtype == kF32 ? with_shape<kF32>(a, run) : with_shape<kBF16>(a, run);
 }
 
 } // namespace cbk
