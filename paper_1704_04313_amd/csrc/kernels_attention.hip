@@ -122,26 +122,35 @@ hipError_t recurrent_any(hipStream_t st, const cbinfer_linear_attention_args &a)
 // ---- prompts: 64 tokens at a time ----------------------------------------------------------------
 // With i and j counting the m tokens of a chunk and S the state in front of it,
 //   O = diag(g^(i+1)) (Q S) + (Q K^T o g^(i-j), i >= j) V        S' = g^m S + K^T diag(g^(m-1-j)) V
-// are matrix products.  A workgroup takes a stream's head and 32 columns of v a wave; each wave keeps its columns of S in the
-// accumulators of the matrix instruction from chunk to chunk, and uses them as an operand as they lie there: the order in
-// which a sum over rows of S runs is free, so Q is read in the order that the accumulators have.  Q, K, V and the
-// scores lie in LDS, the next chunk's are on their way in registers.
+// are matrix products.  A workgroup takes a stream's head and NC times 32 columns of v, two waves for each: one keeps the upper
+// half of the rows of S in the accumulators of the matrix instruction from chunk to chunk, one the lower, and uses them as an
+// operand as they lie there: the order in which a sum over rows of S runs is free, so Q is read in the order that the accumulators
+// have.  The two exchange half of their parts of Q S through LDS and then have 32 queries each.  Q, K, V and
+// the scores lie in LDS, the next chunk's are on their way in registers.
 //
 // bfloat16: what is computed on the way enters a product as a sum of bfloat16 -- scores and states two (16 bits are kept;
 // the output keeps 8), the faded values, from which the state is added up, three (24 bits, exact).  float32: the float32
 // instruction.
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kChunk = 64;
 
+// 32 x 32 and 16 x 16
 __device__ __forceinline__ f32x16 multiply(const u32x4 &a, const u32x4 &b, const f32x16 &c)
 {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 __device__ __forceinline__ f32x16 multiply(float a, float b, const f32x16 &c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 multiply(const u32x4 &a, const u32x4 &b, const f32x4 &c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 multiply(float a, float b, const f32x4 &c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
 // The upper halves of two words: the first in the lower half.
 __device__ __forceinline__ unsigned upper_halves(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
@@ -172,166 +181,196 @@ __device__ __forceinline__ float power(float g, int n)
     return (float)p;
 }
 
-template <int DT, int KT, int NW>
+template <int DT, int KT, int NC, bool OUT>
 struct alignas(16) ChunkLds {
     typedef typename Elem<DT>::type T;
-    static constexpr int K = 32 * KT, V = 32 * NW, PAD = 16 / (int)sizeof(T); // rows 16 bytes longer: 16 lanes reach all banks
-    T q[kChunk][K + PAD], k[kChunk][K + PAD], v[kChunk][V + PAD];
-    T p[DT == kBF16 ? 2 : 1][kChunk][kChunk + PAD]; // scores, by query; bfloat16: in two parts
-    float fade[kChunk + 1];      // g^0 ... g^64
+    static constexpr int K = 32 * KT, V = 32 * NC, PAD = 16 / (int)sizeof(T); // rows 16 bytes longer: 16 lanes reach all banks
+    T k[kChunk][K + PAD], v[kChunk][V + PAD], q[OUT ? kChunk : 1][K + PAD];
+    T p[DT == kBF16 ? 2 : 1][OUT ? kChunk : 1][kChunk + PAD]; // scores, by query; bfloat16: in two parts
+    f32x4 other[OUT ? 2 * NC : 1][4][64]; // a wave's part of Q S for the queries of the wave beside it
+    float fade[kChunk];          // g^1 ... g^64
+    float fade_v[kChunk];        // g^(m-1) ... g^0 of the chunk at hand
     float fade_back[2 * kChunk]; // g^63 ... g^0, then ones
+    int odd[2];                  // whether the chunk, and the next, hold a value that is not finite
 };
 
 // OUT: outputs of the tokens of a part (`per` chunks) of the sequence, from the state in front of it.  Otherwise what those
 // tokens leave in a state of zero, where further tokens follow.  `states`: [stream][head][part][key_size][value_size].
-template <int DT, int KT, int NW, bool OUT>
-__global__ __launch_bounds__(NW * 64) void chunk_kernel(const cbinfer_linear_attention_args a, int slices, int per, int parts, float *states, int whole)
+// WHOLE: rows are pieces of 16 bytes at 16-byte addresses.
+template <int DT, int KT, int NC, bool OUT, bool WHOLE>
+__global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_attention_args a, int slices, int per, int parts, float *states)
 {
     typedef typename Elem<DT>::type T;
-    typedef ChunkLds<DT, KT, NW> Lds;
-    constexpr int E = 16 / (int)sizeof(T), NT = NW * 64; // E: values in 16 bytes
-    constexpr int QP = kChunk * Lds::K / E / NT, VP = kChunk * Lds::V / E / NT; // pieces of 16 bytes a thread
+    typedef ChunkLds<DT, KT, NC, OUT> Lds;
+    constexpr int E = 16 / (int)sizeof(T), NT = NC * 128, KH = KT / 2; // E: values in 16 bytes
+    constexpr int KW = Lds::K / E, VW = Lds::V / E, KR = NT / KW, VR = NT / VW; // pieces of 16 bytes in a row, rows at a time
+    constexpr int KP = kChunk / KR, VP = kChunk / VR;
+    static_assert(KR * KW == NT && VR * VW == NT && KP >= 1 && VP >= 1, "whole rows at a time");
     __shared__ Lds lds;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, side = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, side = lane & 31, half = lane >> 5, low = wave & 1, tile = wave >> 1;
     const int slice = blockIdx.x % slices, bh = blockIdx.x / slices, b = bh / a.heads, h = bh - b * a.heads, hk = h / (a.heads / a.kv_heads);
-    const int part = blockIdx.y, dk = a.key_size, dv = a.value_size, column = slice * Lds::V + wave * 32 + side;
+    const int part = blockIdx.y, dk = a.key_size, dv = a.value_size, column = slice * Lds::V + tile * 32 + side;
     const int n = a.lengths ? min(max(a.lengths[b], 0), a.tokens) : a.tokens;
     const int t0 = part * per * kChunk, t1 = min(n, t0 + per * kChunk);
     T *o = static_cast<T *>(a.o) + b * a.o_stride[0] + h * a.o_stride[2];
     if (OUT) {
         const int end = min(a.tokens, t0 + per * kChunk);
-        for (int64_t t = max(n, t0) + half; t < end; t += 2)
+        for (int64_t t = max(n, t0) + 2 * low + half; t < end; t += 4)
             if (column < dv) o[t * a.o_stride[1] + column] = Elem<DT>::put(0.0f);
         if (t0 >= n) return;
     } else if (t0 + per * kChunk >= n) {
         return;
     }
-    const T *q = static_cast<const T *>(a.q) + b * a.q_stride[0] + h * a.q_stride[2];
-    const T *k = static_cast<const T *>(a.k) + b * a.k_stride[0] + hk * a.k_stride[2];
-    const T *v = static_cast<const T *>(a.v) + b * a.v_stride[0] + hk * a.v_stride[2] + slice * Lds::V;
 
-    // 16 bytes of a row, zeros beyond the tokens and the row
-    auto piece = [&](const T *x, int64_t stride, int t, int at, int size) {
+    // what this thread brings of a chunk: pieces at one place of the row, KR (VR) rows apart
+    const int krow = threadIdx.x / KW, kcol = threadIdx.x % KW * E, vrow = threadIdx.x / VW, vcol = threadIdx.x % VW * E;
+    const int vsize = dv - slice * Lds::V;
+    const T *q = static_cast<const T *>(a.q) + b * a.q_stride[0] + h * a.q_stride[2] + (int64_t)(t0 + krow) * a.q_stride[1] + kcol;
+    const T *k = static_cast<const T *>(a.k) + b * a.k_stride[0] + hk * a.k_stride[2] + (int64_t)(t0 + krow) * a.k_stride[1] + kcol;
+    const T *v = static_cast<const T *>(a.v) + b * a.v_stride[0] + hk * a.v_stride[2] + slice * Lds::V + (int64_t)(t0 + vrow) * a.v_stride[1] + vcol;
+    auto piece = [&](const T *from, bool there, int left) { // left: values up to the row's end
         u32x4 r = {0, 0, 0, 0};
-        if (t < t1 && at < size) {
-            const T *from = x + t * stride + at;
-            if (whole && at + E <= size) {
-                r = *reinterpret_cast<const u32x4 *>(from);
-            } else {
-                union { T e[E]; u32x4 v; } u;
-                u.v = r;
+        if (WHOLE) {
+            if (there && left > 0) r = *reinterpret_cast<const u32x4 *>(from);
+        } else {
+            union { T e[E]; u32x4 v; } u;
+            u.v = r;
 #pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (at + e < size) u.e[e] = from[e];
-                r = u.v;
-            }
+            for (int e = 0; e < E; ++e)
+                if (there && e < left) u.e[e] = from[e];
+            r = u.v;
         }
         return r;
     };
-    u32x4 qr[OUT ? QP : 1], kr[QP], vr[VP];
-    auto load = [&](int t) {
+    u32x4 qr[OUT ? KP : 1], kr[KP], vr[VP];
+    auto load = [&](int tokens) { // those left
 #pragma unroll
-        for (int i = 0; i < QP; ++i) {
-            const int at = i * NT + threadIdx.x, row = at / (Lds::K / E), col = at % (Lds::K / E) * E;
-            if (OUT) qr[OUT ? i : 0] = piece(q, a.q_stride[1], t + row, col, dk);
-            kr[i] = piece(k, a.k_stride[1], t + row, col, dk);
+        for (int i = 0; i < KP; ++i) {
+            if (OUT) qr[OUT ? i : 0] = piece(q + (int64_t)(i * KR) * a.q_stride[1], krow + i * KR < tokens, dk - kcol);
+            kr[i] = piece(k + (int64_t)(i * KR) * a.k_stride[1], krow + i * KR < tokens, dk - kcol);
         }
 #pragma unroll
-        for (int i = 0; i < VP; ++i) {
-            const int at = i * NT + threadIdx.x, row = at / (Lds::V / E), col = at % (Lds::V / E) * E;
-            vr[i] = piece(v, a.v_stride[1], t + row, col, dv - slice * Lds::V);
-        }
+        for (int i = 0; i < VP; ++i) vr[i] = piece(v + (int64_t)(i * VR) * a.v_stride[1], vrow + i * VR < tokens, vsize - vcol);
+        if (OUT) q += kChunk * a.q_stride[1];
+        k += kChunk * a.k_stride[1];
+        v += kChunk * a.v_stride[1];
     };
-    load(t0);
+    load(t1 - t0);
 
     const float g = a.decay[h];
-    for (int i = threadIdx.x; i <= kChunk; i += NT) {
+    if (threadIdx.x < kChunk) {
+        const int i = threadIdx.x;
         const float f = power(g, i);
-        lds.fade[i] = f;
-        if (i < kChunk) lds.fade_back[kChunk - 1 - i] = f;
-        if (i < kChunk) lds.fade_back[kChunk + i] = 1.0f;
+        lds.fade_v[kChunk - 1 - i] = f;
+        lds.fade_back[kChunk - 1 - i] = f;
+        lds.fade_back[kChunk + i] = 1.0f;
+        lds.fade[i] = power(g, i + 1);
     }
+    if (threadIdx.x < 2) lds.odd[threadIdx.x] = 0;
+    if (OUT) // scores of later keys in the tiles that are multiplied all the same
+        for (int i = threadIdx.x; i < 2 * 16 * 16; i += NT) {
+            const int at = i >> 8, row = 32 * at + (i >> 4 & 15), col = 32 * at + 16 + (i & 15);
+            lds.p[0][row][col] = 0;
+            lds.p[DT == kBF16][row][col] = 0;
+        }
 
-    // rows of S: 32 kt + 8 (r / 4) + 4 half + r % 4 for register r; the lane's column
-    f32x16 S[KT];
+    // rows of S: row0 + 32 kt + 8 (r / 4) + r % 4 for register r; the lane's column
+    const int row0 = 32 * KH * low + 4 * half;
+    f32x16 S[KH];
     float *state = a.state + (int64_t)bh * dk * dv;
     {
         const float *from = parts > 1 ? states + ((int64_t)bh * parts + part) * dk * dv : state;
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
+        for (int kt = 0; kt < KH; ++kt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int row = 32 * kt + 8 * (r / 4) + 4 * half + r % 4;
+                const int row = row0 + 32 * kt + 8 * (r / 4) + r % 4;
                 S[kt][r] = OUT && row < dk && column < dv ? from[(int64_t)row * dv + column] : 0.0f;
             }
     }
 
-    for (int t = t0; t < t1; t += kChunk) {
+    int turn = 0;
+    for (int t = t0; t < t1; t += kChunk, turn ^= 1) {
         const int m = min(kChunk, t1 - t);
         __syncthreads(); // the chunk before is done with LDS
 #pragma unroll
-        for (int i = 0; i < QP; ++i) {
-            const int at = i * NT + threadIdx.x, row = at / (Lds::K / E), col = at % (Lds::K / E) * E;
-            *reinterpret_cast<u32x4 *>(&lds.k[row][col]) = kr[i];
+        for (int i = 0; i < KP; ++i) {
+            *reinterpret_cast<u32x4 *>(&lds.k[krow + i * KR][kcol]) = kr[i];
             if (OUT) {
+                const u32x4 &x = qr[OUT ? i : 0];
                 if (DT == kBF16) { // of 16 values, groups of four in the order 0 2 1 3: as the accumulators have S
-                    u32x4 &x = qr[OUT ? i : 0];
-                    const int to = (col & ~15) + (col & 8 ? 4 : 0);
-                    *reinterpret_cast<uint2 *>(&lds.q[row][to]) = make_uint2(x[0], x[1]);
-                    *reinterpret_cast<uint2 *>(&lds.q[row][to + 8]) = make_uint2(x[2], x[3]);
+                    T *to = &lds.q[krow + i * KR][(kcol & ~15) + (kcol & 8 ? 4 : 0)];
+                    *reinterpret_cast<uint2 *>(to) = make_uint2(x[0], x[1]);
+                    *reinterpret_cast<uint2 *>(to + 8) = make_uint2(x[2], x[3]);
                 } else {
-                    *reinterpret_cast<u32x4 *>(&lds.q[row][col]) = qr[OUT ? i : 0];
+                    *reinterpret_cast<u32x4 *>(&lds.q[krow + i * KR][kcol]) = x;
                 }
             }
         }
 #pragma unroll
-        for (int i = 0; i < VP; ++i) {
-            const int at = i * NT + threadIdx.x, row = at / (Lds::V / E), col = at % (Lds::V / E) * E;
-            *reinterpret_cast<u32x4 *>(&lds.v[row][col]) = vr[i];
-        }
-        __syncthreads();
-        if (t + kChunk < t1) load(t + kChunk);
-
-        f32x16 acc[2];
+        for (int i = 0; i < VP; ++i) *reinterpret_cast<u32x4 *>(&lds.v[vrow + i * VR][vcol]) = vr[i];
         if (OUT) {
-            // scores of 32 queries and 32 keys each: keys are the rows, so that a lane has four next to one another
-            for (int tile = wave; tile < 3; tile += NW) {
-                const int j0 = tile == 2 ? 32 : 0, i0 = tile == 0 ? 0 : 32;
-                f32x16 p = {};
+            bool odd = false;
+            if (DT == kBF16) {
+                u16x2 most = {0, 0};
+#pragma unroll
+                for (int i = 0; i < VP; ++i)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, vr[i][w] & 0x7fff7fffu));
+                odd = most[0] >= 0x7f80 || most[1] >= 0x7f80;
+            } else {
+                unsigned most = 0;
+#pragma unroll
+                for (int i = 0; i < VP; ++i)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) most = max(most, vr[i][w] & 0x7fffffffu);
+                odd = most >= 0x7f800000u;
+            }
+            if (odd) lds.odd[turn] = 1;
+        }
+        if (m < kChunk && threadIdx.x < kChunk) lds.fade_v[threadIdx.x] = lds.fade_back[min((int)threadIdx.x + kChunk - m, kChunk - 1)];
+        __syncthreads();
+        if (t + kChunk < t1) load(t1 - t - kChunk);
+
+        f32x16 acc;
+        if (OUT) {
+            if (threadIdx.x == 0) lds.odd[turn ^ 1] = 0;
+            // scores of 16 queries and 16 keys at a time, not of later keys: keys are the rows, so that a lane has four next to one another
+            for (int at = wave; at < 10; at += 2 * NC) {
+                const int it = at < 1 ? 0 : at < 3 ? 1 : at < 6 ? 2 : 3, j0 = 16 * (at - it * (it + 1) / 2), col = lane & 15, quarter = lane >> 4;
+                f32x4 p = {0, 0, 0, 0};
                 if constexpr (DT == kBF16) {
+                    const T *kp = &lds.k[j0 + col][16 * (quarter >> 1) + 4 * (quarter & 1)], *qp = &lds.q[16 * it + col][8 * quarter];
+#pragma unroll
+                    for (int s = 0; s < KT; ++s) {
+                        const uint2 x = *reinterpret_cast<const uint2 *>(kp + 32 * s), y = *reinterpret_cast<const uint2 *>(kp + 32 * s + 8);
+                        p = multiply(u32x4{x.x, x.y, y.x, y.y}, *reinterpret_cast<const u32x4 *>(qp + 32 * s), p);
+                    }
+                } else {
+                    const T *kp = &lds.k[j0 + col][4 * quarter], *qp = &lds.q[16 * it + col][4 * quarter];
 #pragma unroll
                     for (int s = 0; s < 2 * KT; ++s) {
-                        const uint2 x = *reinterpret_cast<const uint2 *>(&lds.k[j0 + side][16 * s + 4 * half]), y = *reinterpret_cast<const uint2 *>(&lds.k[j0 + side][16 * s + 8 + 4 * half]);
-                        p = multiply(u32x4{x.x, x.y, y.x, y.y}, *reinterpret_cast<const u32x4 *>(&lds.q[i0 + side][16 * s + 8 * half]), p);
-                    }
-                } else {
+                        const f32x4 x = *reinterpret_cast<const f32x4 *>(kp + 16 * s), y = *reinterpret_cast<const f32x4 *>(qp + 16 * s);
 #pragma unroll
-                    for (int s = 0; s < 4 * KT; ++s) {
-                        const float4 x = *reinterpret_cast<const float4 *>(&lds.k[j0 + side][8 * s + 4 * half]), y = *reinterpret_cast<const float4 *>(&lds.q[i0 + side][8 * s + 4 * half]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) p = multiply((&x.x)[e], (&y.x)[e], p);
+                        for (int e = 0; e < 4; ++e) p = multiply(x[e], y[e], p);
                     }
                 }
-                const int i = i0 + side;
+                const int i = 16 * it + col, j = j0 + 4 * quarter;
+                const float *fade = lds.fade_back + (kChunk - 1 - i + j);
+                float x[4];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const int j = j0 + 8 * c + 4 * half;
-                    float x[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = i >= j + e ? p[4 * c + e] * lds.fade[max(i - j - e, 0)] : 0.0f;
-                    if constexpr (DT == kBF16) {
-                        *reinterpret_cast<uint2 *>(&lds.p[0][i][j]) = make_uint2(upper_halves(x[0], x[1]), upper_halves(x[2], x[3]));
-                        *reinterpret_cast<uint2 *>(&lds.p[DT == kBF16][i][j]) = make_uint2(bf16_pair(x[0] - cut(x[0]), x[1] - cut(x[1])), bf16_pair(x[2] - cut(x[2]), x[3] - cut(x[3])));
-                    } else {
-                        *reinterpret_cast<float4 *>(&lds.p[0][i][j]) = make_float4(x[0], x[1], x[2], x[3]);
-                    }
+                for (int e = 0; e < 4; ++e) x[e] = i >= j + e ? p[e] * fade[e] : 0.0f;
+                if constexpr (DT == kBF16) {
+                    *reinterpret_cast<uint2 *>(&lds.p[0][i][j]) = make_uint2(upper_halves(x[0], x[1]), upper_halves(x[2], x[3]));
+                    *reinterpret_cast<uint2 *>(&lds.p[DT == kBF16][i][j]) = make_uint2(bf16_pair(x[0] - cut(x[0]), x[1] - cut(x[1])), bf16_pair(x[2] - cut(x[2]), x[3] - cut(x[3])));
+                } else {
+                    *reinterpret_cast<f32x4 *>(&lds.p[0][i][j]) = f32x4{x[0], x[1], x[2], x[3]};
                 }
             }
-            // Q S
-            acc[0] = f32x16{};
-            acc[1] = f32x16{};
+            // this wave's rows of S in Q S
+            f32x16 qs[2] = {};
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
+            for (int kt = 0; kt < KH; ++kt) {
                 if constexpr (DT == kBF16) {
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
@@ -340,123 +379,129 @@ __global__ __launch_bounds__(NW * 64) void chunk_kernel(const cbinfer_linear_att
 #pragma unroll
                         for (int e = 0; e < 8; ++e) x[e] = S[kt][8 * s + e];
                         split(x, y);
-#pragma unroll
-                        for (int it = 0; it < 2; ++it) {
-                            const u32x4 z = *reinterpret_cast<const u32x4 *>(&lds.q[32 * it + side][32 * kt + 16 * s + 8 * half]);
-                            acc[it] = multiply(z, y[0], acc[it]);
-                            acc[it] = multiply(z, y[1], acc[it]);
-                        }
+                        const T *qp = &lds.q[side][32 * (KH * low + kt) + 16 * s + 8 * half];
+                        const u32x4 z0 = *reinterpret_cast<const u32x4 *>(qp), z1 = *reinterpret_cast<const u32x4 *>(qp + 32 * (Lds::K + Lds::PAD));
+                        qs[0] = multiply(z0, y[0], qs[0]);
+                        qs[1] = multiply(z1, y[0], qs[1]);
+                        qs[0] = multiply(z0, y[1], qs[0]);
+                        qs[1] = multiply(z1, y[1], qs[1]);
                     }
                 } else {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
+                    for (int c = 0; c < 4; ++c) {
+                        const T *qp = &lds.q[side][32 * (KH * low + kt) + 8 * c + 4 * half];
+                        const f32x4 z0 = *reinterpret_cast<const f32x4 *>(qp), z1 = *reinterpret_cast<const f32x4 *>(qp + 32 * (Lds::K + Lds::PAD));
 #pragma unroll
-                        for (int it = 0; it < 2; ++it) {
-                            const float4 z = *reinterpret_cast<const float4 *>(&lds.q[32 * it + side][32 * kt + 8 * c + 4 * half]);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[it] = multiply((&z.x)[e], S[kt][4 * c + e], acc[it]);
+                        for (int e = 0; e < 4; ++e) {
+                            qs[0] = multiply(z0[e], S[kt][4 * c + e], qs[0]);
+                            qs[1] = multiply(z1[e], S[kt][4 * c + e], qs[1]);
                         }
+                    }
                 }
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[r] = low ? qs[1][r] : qs[0][r];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                f32x4 x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = low ? qs[0][4 * c + e] : qs[1][4 * c + e];
+                lds.other[wave ^ 1][c][lane] = x;
             }
         }
 
         // the wave's columns of V as the second operand: of 32 tokens by the lane half, 16 values in all
         u32x4 vb[DT == kBF16 ? 4 : 1];
-        float vf[DT == kBF16 ? 1 : 32], poison = 0.0f;
+        float vf[DT == kBF16 ? 1 : 32];
         if constexpr (DT == kBF16) {
             const int in = lane & 15;
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
-                const T *from = &lds.v[16 * s + 8 * half + in / 4][wave * 32 + (lane & 16) + 4 * (in & 3)];
-                const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)from);
-                const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(from + 4 * (Lds::V + Lds::PAD)));
-                const uint2 xu = __builtin_bit_cast(uint2, x), yu = __builtin_bit_cast(uint2, y);
-                vb[s] = u32x4{xu.x, xu.y, yu.x, yu.y};
+                const T *from = &lds.v[16 * s + 8 * half + in / 4][tile * 32 + (lane & 16) + 4 * (in & 3)];
+                const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)from));
+                const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(from + 4 * (Lds::V + Lds::PAD))));
+                vb[s] = u32x4{x.x, x.y, y.x, y.y};
             }
         } else {
 #pragma unroll
             for (int c = 0; c < 8; ++c)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) vf[4 * c + e] = lds.v[8 * c + 4 * half + e][wave * 32 + side];
+                for (int e = 0; e < 4; ++e) vf[4 * c + e] = lds.v[8 * c + 4 * half + e][tile * 32 + side];
         }
         auto value = [&](int s, int e) { return __uint_as_float(e & 1 ? vb[s][e / 2] & 0xffff0000u : vb[s][e / 2] << 16); };
 
         if (OUT) {
-            if constexpr (DT == kBF16) {
+            __syncthreads(); // the scores are there, and the other wave's part
+            const int i0 = 32 * low + 4 * half; // of register r: query i0 + 8 (r / 4) + r % 4
 #pragma unroll
-                for (int s = 0; s < 4; ++s)
+            for (int c = 0; c < 4; ++c) {
+                const f32x4 x = lds.other[wave][c][lane], f = *reinterpret_cast<const f32x4 *>(&lds.fade[i0 + 8 * c]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) poison = __builtin_fmaf(value(s, e), 0.0f, poison);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 32; ++e) poison = __builtin_fmaf(vf[e], 0.0f, poison);
+                for (int e = 0; e < 4; ++e) acc[4 * c + e] = (acc[4 * c + e] + x[e]) * f[e];
             }
-            __syncthreads(); // scores are there
+            if (!lds.odd[turn]) {
+                auto keys = [&](int first) { // 32 of them
+                    if constexpr (DT == kBF16) {
 #pragma unroll
-            for (int it = 0; it < 2; ++it)
+                        for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[it][r] *= lds.fade[32 * it + 8 * (r / 4) + 4 * half + r % 4 + 1];
-            if (!__any(poison != 0.0f)) {
-                if constexpr (DT == kBF16) {
+                            for (int i = 0; i < 2; ++i)
+                                acc = multiply(*reinterpret_cast<const u32x4 *>(&lds.p[DT == kBF16 ? i : 0][32 * low + side][32 * first + 16 * s + 8 * half]), vb[2 * first + s], acc);
+                    } else {
 #pragma unroll
-                    for (int it = 0; it < 2; ++it)
+                        for (int c = 0; c < 4; ++c) {
+                            const f32x4 z = *reinterpret_cast<const f32x4 *>(&lds.p[0][32 * low + side][32 * first + 8 * c + 4 * half]);
 #pragma unroll
-                        for (int s = 0; s < 2 + 2 * it; ++s)
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) acc[it] = multiply(*reinterpret_cast<const u32x4 *>(&lds.p[DT == kBF16 ? i : 0][32 * it + side][16 * s + 8 * half]), vb[s], acc[it]);
-                } else {
-#pragma unroll
-                    for (int it = 0; it < 2; ++it)
-#pragma unroll
-                        for (int c = 0; c < 4 + 4 * it; ++c) {
-                            const float4 z = *reinterpret_cast<const float4 *>(&lds.p[0][32 * it + side][8 * c + 4 * half]);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[it] = multiply((&z.x)[e], vf[4 * c + e], acc[it]);
+                            for (int e = 0; e < 4; ++e) acc = multiply(z[e], vf[16 * first + 4 * c + e], acc);
                         }
-                }
+                    }
+                };
+                keys(0);
+                if (low) keys(1);
             } else { // a value that is not finite: its product with the score 0 of an earlier token must not be added
                 for (int j = 0; j < m; ++j) {
-                    const float x = Elem<DT>::get(lds.v[j][wave * 32 + side]);
+                    const float x = Elem<DT>::get(lds.v[j][tile * 32 + side]);
 #pragma unroll
-                    for (int it = 0; it < 2; ++it)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const int i = 32 * it + 8 * (r / 4) + 4 * half + r % 4;
-                            if (i >= j) {
-                                float p = Elem<DT>::get(lds.p[0][i][j]);
-                                if (DT == kBF16) p += Elem<DT>::get(lds.p[DT == kBF16][i][j]);
-                                acc[it][r] = __builtin_fmaf(p, x, acc[it][r]);
-                            }
+                    for (int r = 0; r < 16; ++r) {
+                        const int i = i0 + 8 * (r / 4) + r % 4;
+                        if (i >= j) {
+                            float p = Elem<DT>::get(lds.p[0][i][j]);
+                            if (DT == kBF16) p += Elem<DT>::get(lds.p[DT == kBF16][i][j]);
+                            acc[r] = __builtin_fmaf(p, x, acc[r]);
                         }
+                    }
                 }
             }
+            T *to = o + (int64_t)(t + i0) * a.o_stride[1] + column;
+            if (m == kChunk && column < dv) {
 #pragma unroll
-            for (int it = 0; it < 2; ++it)
+                for (int r = 0; r < 16; ++r) to[(8 * (r / 4) + r % 4) * a.o_stride[1]] = Elem<DT>::put(a.scale * acc[r]);
+            } else {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int i = 32 * it + 8 * (r / 4) + 4 * half + r % 4;
-                    if (i < m && column < dv) o[(int64_t)(t + i) * a.o_stride[1] + column] = Elem<DT>::put(a.scale * acc[it][r]);
-                }
+                for (int r = 0; r < 16; ++r)
+                    if (i0 + 8 * (r / 4) + r % 4 < m && column < dv) to[(8 * (r / 4) + r % 4) * a.o_stride[1]] = Elem<DT>::put(a.scale * acc[r]);
+            }
         }
 
         // the state behind the chunk
-        const float all = lds.fade[m], *fade = lds.fade_back + kChunk - m; // of token j: g^(m-1-j), and 1 beyond, where values are 0
+        const float all = lds.fade[m - 1];
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
+        for (int kt = 0; kt < KH; ++kt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) S[kt][r] *= all;
         if constexpr (DT == kBF16) {
             const int in = lane & 15;
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
+                const f32x4 f0 = *reinterpret_cast<const f32x4 *>(&lds.fade_v[16 * s + 8 * half]), f1 = *reinterpret_cast<const f32x4 *>(&lds.fade_v[16 * s + 8 * half + 4]);
                 float x[8];
                 u32x4 y[3];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = value(s, e) * fade[16 * s + 8 * half + e];
+                for (int e = 0; e < 8; ++e) x[e] = value(s, e) * (e < 4 ? f0[e % 4] : f1[e % 4]);
                 split(x, y);
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt) {
-                    const T *from = &lds.k[16 * s + 8 * half + in / 4][32 * kt + (lane & 16) + 4 * (in & 3)];
+                for (int kt = 0; kt < KH; ++kt) {
+                    const T *from = &lds.k[16 * s + 8 * half + in / 4][32 * (KH * low + kt) + (lane & 16) + 4 * (in & 3)];
                     const uint2 p = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)from));
                     const uint2 u = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(from + 4 * (Lds::K + Lds::PAD))));
 #pragma unroll
@@ -465,24 +510,25 @@ __global__ __launch_bounds__(NW * 64) void chunk_kernel(const cbinfer_linear_att
             }
         } else {
 #pragma unroll
-            for (int c = 0; c < 8; ++c)
+            for (int c = 0; c < 8; ++c) {
+                const f32x4 f = *reinterpret_cast<const f32x4 *>(&lds.fade_v[8 * c + 4 * half]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int j = 8 * c + 4 * half + e;
-                    const float x = vf[4 * c + e] * fade[j];
+                    const float x = vf[4 * c + e] * f[e];
 #pragma unroll
-                    for (int kt = 0; kt < KT; ++kt) S[kt] = multiply(lds.k[j][32 * kt + side], x, S[kt]);
+                    for (int kt = 0; kt < KH; ++kt) S[kt] = multiply(lds.k[8 * c + 4 * half + e][32 * (KH * low + kt) + side], x, S[kt]);
                 }
+            }
         }
     }
 
     float *to = OUT ? state : states + ((int64_t)bh * parts + part + 1) * dk * dv;
     if (!OUT || t1 == n) // the part with the last token
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
+        for (int kt = 0; kt < KH; ++kt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int row = 32 * kt + 8 * (r / 4) + 4 * half + r % 4;
+                const int row = row0 + 32 * kt + 8 * (r / 4) + r % 4;
                 if (row < dk && column < dv) to[(int64_t)row * dv + column] = S[kt][r];
             }
 }
@@ -495,10 +541,17 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const cbinfer_linear_at
     const int n = a.lengths ? min(max(a.lengths[b], 0), a.tokens) : a.tokens;
     const float g = power(a.decay[bh - b * a.heads], per * kChunk);
     float *s = states + (int64_t)bh * parts * size + at, x = a.state[(int64_t)bh * size + at];
+    const int last = (int)min((int64_t)parts, ((int64_t)n + per * kChunk - 1) / (per * kChunk)); // parts with tokens
     s[0] = x;
-    for (int p = 1; p < parts && (int64_t)p * per * kChunk < n; ++p) {
-        x = __builtin_fmaf(g, x, s[(int64_t)p * size]);
-        s[(int64_t)p * size] = x;
+    for (int p0 = 1; p0 < last; p0 += 8) { // eight loads on their way at a time
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = p0 + i < last ? s[(int64_t)(p0 + i) * size] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x = __builtin_fmaf(g, x, v[i]);
+            if (p0 + i < last) s[(int64_t)(p0 + i) * size] = x;
+        }
     }
 }
 
@@ -523,35 +576,41 @@ Plan plan(const cbinfer_linear_attention_args &a)
     return p;
 }
 
-template <int DT, int KT, int NW>
+template <int DT, int KT, int NC, bool WHOLE>
 hipError_t chunked(hipStream_t st, const cbinfer_linear_attention_args &a, const Plan &p)
 {
-    const size_t e = DT == kF32 ? 4 : 2;
-    auto fits = [&](const void *x, const int64_t *stride) {
-        for (int i = 0; i < 3; ++i)
-            if (stride[i] * e % 16) return 0;
-        return reinterpret_cast<uintptr_t>(x) % 16 == 0 ? 1 : 0;
-    };
-    const int whole = fits(a.q, a.q_stride) & fits(a.k, a.k_stride) & fits(a.v, a.v_stride);
     float *states = static_cast<float *>(a.workspace);
     const unsigned groups = (unsigned)(a.streams * a.heads * p.slices);
     if (p.parts > 1) {
-        chunk_kernel<DT, KT, NW, false><<<dim3(groups, p.parts - 1), NW * 64, 0, st>>>(a, p.slices, p.per, p.parts, states, whole);
+        chunk_kernel<DT, KT, NC, false, WHOLE><<<dim3(groups, p.parts - 1), NC * 128, 0, st>>>(a, p.slices, p.per, p.parts, states);
         if (hipError_t err = hipGetLastError()) return err;
         join_parts_kernel<<<dim3((a.key_size * a.value_size + 255) / 256, a.streams * a.heads), 256, 0, st>>>(a, p.per, p.parts, states);
         if (hipError_t err = hipGetLastError()) return err;
     }
-    chunk_kernel<DT, KT, NW, true><<<dim3(groups, p.parts), NW * 64, 0, st>>>(a, p.slices, p.per, p.parts, states, whole);
+    chunk_kernel<DT, KT, NC, true, WHOLE><<<dim3(groups, p.parts), NC * 128, 0, st>>>(a, p.slices, p.per, p.parts, states);
     return hipGetLastError();
+}
+
+template <int DT, bool WHOLE>
+hipError_t chunked_any(hipStream_t st, const cbinfer_linear_attention_args &a, const Plan &p)
+{
+    if (a.key_size <= 64) return p.tiles == 2 ? chunked<DT, 2, 2, WHOLE>(st, a, p) : chunked<DT, 2, 4, WHOLE>(st, a, p);
+    if (a.key_size <= 128) return p.tiles == 2 ? chunked<DT, 4, 2, WHOLE>(st, a, p) : chunked<DT, 4, 4, WHOLE>(st, a, p);
+    if constexpr (DT == kBF16) return chunked<DT, 8, 4, WHOLE>(st, a, p);
+    return hipErrorInvalidValue;
 }
 
 template <int DT>
 hipError_t chunked_any(hipStream_t st, const cbinfer_linear_attention_args &a, const Plan &p)
 {
-    if (a.key_size <= 64) return p.tiles == 2 ? chunked<DT, 2, 2>(st, a, p) : chunked<DT, 2, 4>(st, a, p);
-    if (a.key_size <= 128) return p.tiles == 2 ? chunked<DT, 4, 2>(st, a, p) : chunked<DT, 4, 4>(st, a, p);
-    if constexpr (DT == kBF16) return chunked<DT, 8, 4>(st, a, p);
-    return hipErrorInvalidValue;
+    const size_t e = DT == kF32 ? 4 : 2;
+    auto fits = [&](const void *x, const int64_t *stride, int size) {
+        for (int i = 0; i < 3; ++i)
+            if (stride[i] * e % 16) return false;
+        return reinterpret_cast<uintptr_t>(x) % 16 == 0 && size * e % 16 == 0;
+    };
+    const bool whole = fits(a.q, a.q_stride, a.key_size) && fits(a.k, a.k_stride, a.key_size) && fits(a.v, a.v_stride, a.value_size);
+    return whole ? chunked_any<DT, true>(st, a, p) : chunked_any<DT, false>(st, a, p);
 }
 
 } // namespace
