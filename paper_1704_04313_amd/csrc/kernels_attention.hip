@@ -4,7 +4,6 @@
 #include "tokens.h"
 
 #include <algorithm>
-#include <cstdlib>
 
 namespace cbk {
 namespace {
@@ -140,6 +139,12 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kChunk = 64;
 
+// Memory with its size: what is read beyond it is zero, what is written there is dropped, so that ragged edges take no branches
+// (code that runs once is fetched from far away, and costs more than it executes).  Offsets in bytes; kBeyond is beyond any.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+constexpr unsigned kBeyond = 0x80000000u;
+__device__ __forceinline__ Buffer buffer(const void *p, unsigned bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, bytes, 0x00027000); }
+
 // 32 x 32 and 16 x 16
 __device__ __forceinline__ f32x16 multiply(const u32x4 &a, const u32x4 &b, const f32x16 &c)
 {
@@ -184,8 +189,11 @@ __device__ __forceinline__ float power(float g, int n)
 template <int DT, int KT, int NC, bool OUT>
 struct alignas(16) ChunkLds {
     typedef typename Elem<DT>::type T;
-    static constexpr int K = 32 * KT, V = 32 * NC, PAD = 16 / (int)sizeof(T); // rows 16 bytes longer: 16 lanes reach all banks
-    T k[kChunk][K + PAD], v[kChunk][V + PAD], q[OUT ? kChunk : 1][K + PAD];
+    // Rows are longer so that the lanes of an access reach different banks: 16 bytes where each lane reads 16 of a row of its own,
+    // 64 where four rows are read across (bfloat16 K and V, transposed on the way).
+    static constexpr int K = 32 * KT, V = 32 * NC, PAD = 16 / (int)sizeof(T), ACROSS = DT == kBF16 ? 32 : PAD;
+    static constexpr int KPAD = OUT ? PAD : ACROSS; // both ways where there are scores: 16 bytes are the better choice (49 us against 54)
+    T k[kChunk][K + KPAD], v[kChunk][V + ACROSS], q[OUT ? kChunk : 1][K + PAD];
     T p[DT == kBF16 ? 2 : 1][OUT ? kChunk : 1][kChunk + PAD]; // scores, by query; bfloat16: in two parts
     f32x4 other[OUT ? 2 * NC : 1][4][64]; // a wave's part of Q S for the queries of the wave beside it
     float fade[kChunk];          // g^1 ... g^64
@@ -225,33 +233,36 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
     // what this thread brings of a chunk: pieces at one place of the row, KR (VR) rows apart
     const int krow = threadIdx.x / KW, kcol = threadIdx.x % KW * E, vrow = threadIdx.x / VW, vcol = threadIdx.x % VW * E;
     const int vsize = dv - slice * Lds::V;
-    const T *q = static_cast<const T *>(a.q) + b * a.q_stride[0] + h * a.q_stride[2] + (int64_t)(t0 + krow) * a.q_stride[1] + kcol;
-    const T *k = static_cast<const T *>(a.k) + b * a.k_stride[0] + hk * a.k_stride[2] + (int64_t)(t0 + krow) * a.k_stride[1] + kcol;
-    const T *v = static_cast<const T *>(a.v) + b * a.v_stride[0] + hk * a.v_stride[2] + slice * Lds::V + (int64_t)(t0 + vrow) * a.v_stride[1] + vcol;
-    auto piece = [&](const T *from, bool there, int left) { // left: values up to the row's end
-        u32x4 r = {0, 0, 0, 0};
-        if (WHOLE) {
-            if (there && left > 0) r = *reinterpret_cast<const u32x4 *>(from);
-        } else {
-            union { T e[E]; u32x4 v; } u;
-            u.v = r;
+    const T *q = static_cast<const T *>(a.q) + b * a.q_stride[0] + h * a.q_stride[2] + t0 * a.q_stride[1];
+    const T *k = static_cast<const T *>(a.k) + b * a.k_stride[0] + hk * a.k_stride[2] + t0 * a.k_stride[1];
+    const T *v = static_cast<const T *>(a.v) + b * a.v_stride[0] + hk * a.v_stride[2] + t0 * a.v_stride[1] + slice * Lds::V;
+    auto rows = [&](auto &r, const T *from, int64_t stride, int tokens, int row, int col, int step, int size) {
+        constexpr int N = sizeof(r) / sizeof(r[0]);
+        if constexpr (WHOLE) {
+            const unsigned each = (unsigned)stride * sizeof(T);
+            const Buffer x = buffer(from, (min(tokens, kChunk) - 1) * each + size * sizeof(T));
+            unsigned at = col < size ? row * each + col * (unsigned)sizeof(T) : kBeyond;
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (there && e < left) u.e[e] = from[e];
-            r = u.v;
+            for (int i = 0; i < N; ++i, at += step * each) r[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(x, at, 0, 0));
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                union { T e[E]; u32x4 v; } u;
+                u.v = u32x4{0, 0, 0, 0};
+                const T *p = from + (row + i * step) * stride + col;
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (row + i * step < tokens && col + e < size) u.e[e] = p[e];
+                r[i] = u.v;
+            }
         }
-        return r;
     };
     u32x4 qr[OUT ? KP : 1], kr[KP], vr[VP];
     auto load = [&](int tokens) { // those left
-#pragma unroll
-        for (int i = 0; i < KP; ++i) {
-            if (OUT) qr[OUT ? i : 0] = piece(q + (int64_t)(i * KR) * a.q_stride[1], krow + i * KR < tokens, dk - kcol);
-            kr[i] = piece(k + (int64_t)(i * KR) * a.k_stride[1], krow + i * KR < tokens, dk - kcol);
-        }
-#pragma unroll
-        for (int i = 0; i < VP; ++i) vr[i] = piece(v + (int64_t)(i * VR) * a.v_stride[1], vrow + i * VR < tokens, vsize - vcol);
-        if (OUT) q += kChunk * a.q_stride[1];
+        if constexpr (OUT) rows(qr, q, a.q_stride[1], tokens, krow, kcol, KR, dk);
+        rows(kr, k, a.k_stride[1], tokens, krow, kcol, KR, dk);
+        rows(vr, v, a.v_stride[1], tokens, vrow, vcol, VR, vsize);
+        q += kChunk * a.q_stride[1];
         k += kChunk * a.k_stride[1];
         v += kChunk * a.v_stride[1];
     };
@@ -276,17 +287,16 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
 
     // rows of S: row0 + 32 kt + 8 (r / 4) + r % 4 for register r; the lane's column
     const int row0 = 32 * KH * low + 4 * half;
-    f32x16 S[KH];
+    const unsigned state_bytes = (unsigned)(dk * dv) * 4, state_at = column < dv ? (unsigned)(row0 * dv + column) * 4 : kBeyond;
+    auto place = [&](int kt, int r) { return state_at + (unsigned)((32 * kt + 8 * (r / 4) + r % 4) * dv) * 4; };
+    f32x16 S[KH] = {};
     float *state = a.state + (int64_t)bh * dk * dv;
-    {
-        const float *from = parts > 1 ? states + ((int64_t)bh * parts + part) * dk * dv : state;
+    if (OUT) {
+        const Buffer from = buffer(parts > 1 ? states + ((int64_t)bh * parts + part) * dk * dv : state, state_bytes);
 #pragma unroll
         for (int kt = 0; kt < KH; ++kt)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int row = row0 + 32 * kt + 8 * (r / 4) + r % 4;
-                S[kt][r] = OUT && row < dk && column < dv ? from[(int64_t)row * dv + column] : 0.0f;
-            }
+            for (int r = 0; r < 16; ++r) S[kt][r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(from, place(kt, r), 0, 0));
     }
 
     int turn = 0;
@@ -341,14 +351,14 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
                 f32x4 p = {0, 0, 0, 0};
                 if constexpr (DT == kBF16) {
                     const T *kp = &lds.k[j0 + col][16 * (quarter >> 1) + 4 * (quarter & 1)], *qp = &lds.q[16 * it + col][8 * quarter];
-#pragma unroll
+#pragma unroll 4
                     for (int s = 0; s < KT; ++s) {
                         const uint2 x = *reinterpret_cast<const uint2 *>(kp + 32 * s), y = *reinterpret_cast<const uint2 *>(kp + 32 * s + 8);
                         p = multiply(u32x4{x.x, x.y, y.x, y.y}, *reinterpret_cast<const u32x4 *>(qp + 32 * s), p);
                     }
                 } else {
                     const T *kp = &lds.k[j0 + col][4 * quarter], *qp = &lds.q[16 * it + col][4 * quarter];
-#pragma unroll
+#pragma unroll 4
                     for (int s = 0; s < 2 * KT; ++s) {
                         const f32x4 x = *reinterpret_cast<const f32x4 *>(kp + 16 * s), y = *reinterpret_cast<const f32x4 *>(qp + 16 * s);
 #pragma unroll
@@ -410,26 +420,30 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
             }
         }
 
-        // the wave's columns of V as the second operand: of 32 tokens by the lane half, 16 values in all
-        u32x4 vb[DT == kBF16 ? 4 : 1];
-        float vf[DT == kBF16 ? 1 : 32];
-        if constexpr (DT == kBF16) {
+        // the wave's columns of V as the second operand: bfloat16 of 16 tokens from 16 s on, by the lane half; float32 of 8 from 8 c on
+        auto v16 = [&](int s) {
             const int in = lane & 15;
+            const T *from = &lds.v[16 * s + 8 * half + in / 4][tile * 32 + (lane & 16) + 4 * (in & 3)];
+            const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)from));
+            const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(from + 4 * (Lds::V + Lds::ACROSS))));
+            return u32x4{x.x, x.y, y.x, y.y};
+        };
+        auto v8 = [&](int c) {
+            f32x4 x;
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const T *from = &lds.v[16 * s + 8 * half + in / 4][tile * 32 + (lane & 16) + 4 * (in & 3)];
-                const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)from));
-                const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(from + 4 * (Lds::V + Lds::PAD))));
-                vb[s] = u32x4{x.x, x.y, y.x, y.y};
-            }
-        } else {
-#pragma unroll
-            for (int c = 0; c < 8; ++c)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) vf[4 * c + e] = lds.v[8 * c + 4 * half + e][tile * 32 + side];
-        }
-        auto value = [&](int s, int e) { return __uint_as_float(e & 1 ? vb[s][e / 2] & 0xffff0000u : vb[s][e / 2] << 16); };
+            for (int e = 0; e < 4; ++e) x[e] = Elem<DT>::get(lds.v[8 * c + 4 * half + e][tile * 32 + side]);
+            return x;
+        };
 
+        // 16 tokens of V as they fade up to the chunk's end, in three parts
+        auto fading = [&](int s, u32x4 (&y)[3]) {
+            const f32x4 f0 = *reinterpret_cast<const f32x4 *>(&lds.fade_v[16 * s + 8 * half]), f1 = *reinterpret_cast<const f32x4 *>(&lds.fade_v[16 * s + 8 * half + 4]);
+            const u32x4 vb = v16(s);
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(e & 1 ? vb[e / 2] & 0xffff0000u : vb[e / 2] << 16) * (e < 4 ? f0[e % 4] : f1[e % 4]);
+            split(x, y);
+        };
         if (OUT) {
             __syncthreads(); // the scores are there, and the other wave's part
             const int i0 = 32 * low + 4 * half; // of register r: query i0 + 8 (r / 4) + r % 4
@@ -440,24 +454,21 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
                 for (int e = 0; e < 4; ++e) acc[4 * c + e] = (acc[4 * c + e] + x[e]) * f[e];
             }
             if (!lds.odd[turn]) {
-                auto keys = [&](int first) { // 32 of them
-                    if constexpr (DT == kBF16) {
+                if constexpr (DT == kBF16) {
+#pragma unroll 4
+                    for (int s = 0; s < 2 + 2 * low; ++s) {
+                        const u32x4 y = v16(s);
 #pragma unroll
-                        for (int s = 0; s < 2; ++s)
-#pragma unroll
-                            for (int i = 0; i < 2; ++i)
-                                acc = multiply(*reinterpret_cast<const u32x4 *>(&lds.p[DT == kBF16 ? i : 0][32 * low + side][32 * first + 16 * s + 8 * half]), vb[2 * first + s], acc);
-                    } else {
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const f32x4 z = *reinterpret_cast<const f32x4 *>(&lds.p[0][32 * low + side][32 * first + 8 * c + 4 * half]);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc = multiply(z[e], vf[16 * first + 4 * c + e], acc);
-                        }
+                        for (int i = 0; i < 2; ++i) acc = multiply(*reinterpret_cast<const u32x4 *>(&lds.p[DT == kBF16 ? i : 0][32 * low + side][16 * s + 8 * half]), y, acc);
                     }
-                };
-                keys(0);
-                if (low) keys(1);
+                } else {
+#pragma unroll 4
+                    for (int c = 0; c < 4 + 4 * low; ++c) {
+                        const f32x4 z = *reinterpret_cast<const f32x4 *>(&lds.p[0][32 * low + side][8 * c + 4 * half]), y = v8(c);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc = multiply(z[e], y[e], acc);
+                    }
+                }
             } else { // a value that is not finite: its product with the score 0 of an earlier token must not be added
                 for (int j = 0; j < m; ++j) {
                     const float x = Elem<DT>::get(lds.v[j][tile * 32 + side]);
@@ -472,11 +483,19 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
                     }
                 }
             }
-            T *to = o + (int64_t)(t + i0) * a.o_stride[1] + column;
-            if (m == kChunk && column < dv) {
+            if constexpr (WHOLE) {
+                const unsigned each = (unsigned)a.o_stride[1] * sizeof(T), from = column < dv ? i0 * each + column * (unsigned)sizeof(T) : kBeyond;
+                const Buffer to = buffer(o + t * a.o_stride[1], (m - 1) * each + dv * sizeof(T));
 #pragma unroll
-                for (int r = 0; r < 16; ++r) to[(8 * (r / 4) + r % 4) * a.o_stride[1]] = Elem<DT>::put(a.scale * acc[r]);
+                for (int r = 0; r < 16; ++r) {
+                    const unsigned at = from + (8 * (r / 4) + r % 4) * each;
+                    if constexpr (DT == kBF16)
+                        __builtin_amdgcn_raw_buffer_store_b16(Elem<DT>::put(a.scale * acc[r]), to, at, 0, 0);
+                    else
+                        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(a.scale * acc[r]), to, at, 0, 0);
+                }
             } else {
+                T *to = o + (int64_t)(t + i0) * a.o_stride[1] + column;
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     if (i0 + 8 * (r / 4) + r % 4 < m && column < dv) to[(8 * (r / 4) + r % 4) * a.o_stride[1]] = Elem<DT>::put(a.scale * acc[r]);
@@ -491,30 +510,26 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
             for (int r = 0; r < 16; ++r) S[kt][r] *= all;
         if constexpr (DT == kBF16) {
             const int in = lane & 15;
-#pragma unroll
+#pragma unroll 4
             for (int s = 0; s < 4; ++s) {
-                const f32x4 f0 = *reinterpret_cast<const f32x4 *>(&lds.fade_v[16 * s + 8 * half]), f1 = *reinterpret_cast<const f32x4 *>(&lds.fade_v[16 * s + 8 * half + 4]);
-                float x[8];
                 u32x4 y[3];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = value(s, e) * (e < 4 ? f0[e % 4] : f1[e % 4]);
-                split(x, y);
+                fading(s, y);
 #pragma unroll
                 for (int kt = 0; kt < KH; ++kt) {
                     const T *from = &lds.k[16 * s + 8 * half + in / 4][32 * (KH * low + kt) + (lane & 16) + 4 * (in & 3)];
                     const uint2 p = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)from));
-                    const uint2 u = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(from + 4 * (Lds::K + Lds::PAD))));
+                    const uint2 u = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(from + 4 * (Lds::K + Lds::KPAD))));
 #pragma unroll
                     for (int i = 0; i < 3; ++i) S[kt] = multiply(u32x4{p.x, p.y, u.x, u.y}, y[i], S[kt]);
                 }
             }
         } else {
-#pragma unroll
+#pragma unroll 4
             for (int c = 0; c < 8; ++c) {
-                const f32x4 f = *reinterpret_cast<const f32x4 *>(&lds.fade_v[8 * c + 4 * half]);
+                const f32x4 f = *reinterpret_cast<const f32x4 *>(&lds.fade_v[8 * c + 4 * half]), y = v8(c);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float x = vf[4 * c + e] * f[e];
+                    const float x = y[e] * f[e];
 #pragma unroll
                     for (int kt = 0; kt < KH; ++kt) S[kt] = multiply(lds.k[8 * c + 4 * half + e][32 * (KH * low + kt) + side], x, S[kt]);
                 }
@@ -522,15 +537,13 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
         }
     }
 
-    float *to = OUT ? state : states + ((int64_t)bh * parts + part + 1) * dk * dv;
-    if (!OUT || t1 == n) // the part with the last token
+    if (!OUT || t1 == n) { // the part with the last token
+        const Buffer to = buffer(OUT ? state : states + ((int64_t)bh * parts + part + 1) * dk * dv, state_bytes);
 #pragma unroll
         for (int kt = 0; kt < KH; ++kt)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int row = row0 + 32 * kt + 8 * (r / 4) + r % 4;
-                if (row < dk && column < dv) to[(int64_t)row * dv + column] = S[kt][r];
-            }
+            for (int r = 0; r < 16; ++r) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S[kt][r]), to, place(kt, r), 0, 0);
+    }
 }
 
 // What the parts of a sequence leave by themselves (places 1, 2, ...) becomes the states in front of the parts.
@@ -569,8 +582,10 @@ Plan plan(const cbinfer_linear_attention_args &a)
     p.tiles = tiles <= 2 && a.key_size <= 128 ? 2 : 4;
     p.slices = (tiles + p.tiles - 1) / p.tiles;
     const int64_t groups = (int64_t)a.streams * a.heads * p.slices, chunks = (a.tokens + kChunk - 1) / kChunk;
-    static const int TG = getenv("CBG") ? atoi(getenv("CBG")) : 512;
-    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(chunks / 2, TG / std::max<int64_t>(groups, 1)));
+    // Parts until every compute unit has a workgroup; their keys and values are read twice.  us for 8192 tokens, 16 heads of 128: 8 parts 119,
+    // 16 78, 32 93.  Streams of different lengths leave compute units idle: twice as many (12 streams of up to 1023 tokens, 6 heads,
+    // float32: 3 parts 83, 7 70).
+    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(chunks / 2, (a.lengths ? 512 : 256) / std::max<int64_t>(groups, 1)));
     p.per = (int)((chunks + p.parts - 1) / p.parts);
     p.parts = (int)((chunks + p.per - 1) / p.per);
     return p;
@@ -604,12 +619,14 @@ template <int DT>
 hipError_t chunked_any(hipStream_t st, const cbinfer_linear_attention_args &a, const Plan &p)
 {
     const size_t e = DT == kF32 ? 4 : 2;
+    // rows at 16-byte addresses, those of a chunk in order and within the 31 bits of a buffer's offsets
     auto fits = [&](const void *x, const int64_t *stride, int size) {
         for (int i = 0; i < 3; ++i)
             if (stride[i] * e % 16) return false;
-        return reinterpret_cast<uintptr_t>(x) % 16 == 0 && size * e % 16 == 0;
+        return reinterpret_cast<uintptr_t>(x) % 16 == 0 && size * e % 16 == 0 && stride[1] >= size && stride[1] < (1 << 30) / (int64_t)(kChunk * e);
     };
-    const bool whole = fits(a.q, a.q_stride, a.key_size) && fits(a.k, a.k_stride, a.key_size) && fits(a.v, a.v_stride, a.value_size);
+    const bool whole = fits(a.q, a.q_stride, a.key_size) && fits(a.k, a.k_stride, a.key_size) && fits(a.v, a.v_stride, a.value_size) &&
+                       fits(a.o, a.o_stride, a.value_size);
     return whole ? chunked_any<DT, true>(st, a, p) : chunked_any<DT, false>(st, a, p);
 }
 
