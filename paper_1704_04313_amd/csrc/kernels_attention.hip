@@ -455,14 +455,14 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
             }
             if (!lds.odd[turn]) {
                 if constexpr (DT == kBF16) {
-#pragma unroll 4
+#pragma unroll 2
                     for (int s = 0; s < 2 + 2 * low; ++s) {
                         const u32x4 y = v16(s);
 #pragma unroll
                         for (int i = 0; i < 2; ++i) acc = multiply(*reinterpret_cast<const u32x4 *>(&lds.p[DT == kBF16 ? i : 0][32 * low + side][16 * s + 8 * half]), y, acc);
                     }
                 } else {
-#pragma unroll 4
+#pragma unroll 2
                     for (int c = 0; c < 4 + 4 * low; ++c) {
                         const f32x4 z = *reinterpret_cast<const f32x4 *>(&lds.p[0][32 * low + side][8 * c + 4 * half]), y = v8(c);
 #pragma unroll
