@@ -191,27 +191,32 @@ def log_probs(scores, labels=None, *, dim: int = 1, top: int = 0) -> LogProbs:
     a.classes, a.class_stride = shape[dim], strides[dim]
     before, behind = shape[:dim], shape[dim + 1:]
     cut = dim
-    if 0 in before or 0 in behind:
+    count = scores.numel()
+    if count == 0:
         a.outer = a.inner = 0
+    elif a.classes > 1 and scores.is_contiguous():  # (the stride of an axis of one says nothing)
+        a.inner, a.inner_stride = strides[dim], 1
+        a.outer_stride = a.classes * strides[dim]
+        a.outer = count // a.outer_stride
     else:
         (a.outer, a.outer_stride), (a.inner, a.inner_stride), cut = _positions(before, strides[:dim], behind, strides[dim + 1:])
     a.scores = scores.data_ptr()
     rest = before + behind
     label = values = index = None
+    entropy = torch.empty(rest, dtype=torch.float32, device=device)
     if labels is not None:
         if labels.shape != rest:
             _refuse("labels must have the shape of the scores without the classes, %s (got %s)" % (tuple(rest), tuple(labels.shape)))
         if labels.dtype not in (torch.int32, torch.int64) or not labels.is_contiguous():
             _refuse("labels must be contiguous int32 or int64")
         _same_device(labels, device, "labels")
-        label = torch.empty(rest, dtype=torch.float32, device=device)
+        label = torch.empty_like(entropy)
         a.label_bytes = 4 if labels.dtype == torch.int32 else 8
         a.labels, a.label = labels.data_ptr(), label.data_ptr()
-    entropy = torch.empty(rest, dtype=torch.float32, device=device)
     a.entropy = entropy.data_ptr()
     if top:
         values = torch.empty(rest[:cut] + (top,) + rest[cut:], dtype=torch.float32, device=device)
-        index = torch.empty(rest[:cut] + (top,) + rest[cut:], dtype=torch.int32, device=device)
+        index = torch.empty_like(values, dtype=torch.int32)
         a.top_values, a.top_index = values.data_ptr(), index.data_ptr()
     keep = _workspace(a, lib.cbinfer_log_probs_workspace_bytes(a), device)  # noqa: F841
     rc = lib.cbinfer_log_probs(a, _stream(device))
