@@ -365,8 +365,8 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void rows_kernel(cons
             for (int e = 0; e < V; ++e) add(t, v[e]);
         }
         if (!k) continue;
-        if (round == again) { // rounds 0, 3, 15, 63, ...: what a round wants in the mean falls with the scores that the bound has seen
-            again = 4 * again + 3;
+        if (round == again) { // rounds 0, 1, 3, 7, ...: what a round wants in the mean falls with the scores that the bound has seen
+            again = 2 * again + 1;
             float top = t.m == kLowest ? most : t.m; // the largest so far; of scores of -inf t.m says nothing
             if (WAVES > 1) {
                 shared[threadIdx.x] = top;
@@ -380,27 +380,39 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void rows_kernel(cons
         const unsigned long long hit = __ballot(b.any_wanted(most));
         if (!hit) continue;
         if (__popcll(hit) > 32) b.bound(most); // scores that rise
-#pragma nounroll
-        for (int u = 0; u < U; ++u) { // one place in the code: the units move past it
-            unsigned long long m = __ballot(b.any_wanted(largest[0]) && u0 + u * NT + thread < end);
-            while (m) { // a lane's unit, a score a lane
-                const int l = __ffsll((long long)m) - 1;
-                m &= m - 1;
-                uint4 unit;
-                unit.x = __builtin_amdgcn_readlane(raw[0].x, l);
-                unit.y = __builtin_amdgcn_readlane(raw[0].y, l);
-                unit.z = __builtin_amdgcn_readlane(raw[0].z, l);
-                unit.w = __builtin_amdgcn_readlane(raw[0].w, l);
-                const int word = lane / (V / 4);
-                const unsigned w = word == 0 ? unit.x : word == 1 ? unit.y : word == 2 ? unit.z : unit.w;
-                const float x = __uint_as_float(DT == kF32 ? w : lane & 1 ? w & 0xffff0000u : w << 16);
-                b.offer({x, head + (u0 + u * NT + thread - lane + l) * V + lane}, lane < V);
-            }
+        unsigned long long units[U], left = 0; // lanes whose unit may hold one
 #pragma unroll
-            for (int j = 0; j + 1 < U; ++j) {
-                raw[j] = raw[j + 1];
-                largest[j] = largest[j + 1];
+        for (int u = 0; u < U; ++u) {
+            units[u] = __ballot(b.any_wanted(largest[u]) && u0 + u * NT + thread < end);
+            left |= units[u];
+        }
+        while (left) { // a lane's unit, a score a lane; one place in the code for all of them
+            unsigned long long m = units[U - 1];
+            uint4 unit = raw[U - 1];
+            int u = U - 1;
+#pragma unroll
+            for (int j = U - 2; j >= 0; --j)
+                if (units[j]) {
+                    m = units[j];
+                    unit = raw[j];
+                    u = j;
+                }
+            const int l = __ffsll((long long)m) - 1;
+            m &= m - 1;
+            left = 0;
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                if (j == u) units[j] = m;
+                left |= units[j];
             }
+            unit.x = __builtin_amdgcn_readlane(unit.x, l);
+            unit.y = __builtin_amdgcn_readlane(unit.y, l);
+            unit.z = __builtin_amdgcn_readlane(unit.z, l);
+            unit.w = __builtin_amdgcn_readlane(unit.w, l);
+            const int word = lane / (V / 4);
+            const unsigned w = word == 0 ? unit.x : word == 1 ? unit.y : word == 2 ? unit.z : unit.w;
+            const float x = __uint_as_float(DT == kF32 ? w : lane & 1 ? w & 0xffff0000u : w << 16);
+            b.offer({x, head + (u0 + u * NT + thread - lane + l) * V + lane}, lane < V);
         }
     }
     if (segment == segments - 1) few(tail, n);
@@ -639,9 +651,9 @@ Plan plan(const cbinfer_log_probs_args &a)
         // us a call, 4096 rows of 1000 bfloat16: a wave each 17, four waves each 32
         if (a.classes <= 2048) return p;
         p.waves = 4;
-        // Few long rows are cut into segments of one round of loads at least, up to 1024 workgroups, and joined by a second launch.
-        // 64 rows of 100003 bfloat16: 29 us whole, 18 in 12 segments and more, join included; one of 131071: 28 and 18.
-        const int64_t rounds = a.classes / (4 * 64 * 4 * (a.dtype == kF32 ? 4 : 8)), segments = std::min<int64_t>({rounds, 64, 1024 / std::max<int64_t>(positions, 1)});
+        // Few long rows are cut into segments of one round of loads, up to 1024 workgroups, and joined by a second launch.
+        // 64 rows of 100003 bfloat16: 29 us whole, 18 in segments, join included; one of 131071: 28 and 14.
+        const int64_t round = 4 * 64 * 4 * (a.dtype == kF32 ? 4 : 8), segments = std::min<int64_t>({(a.classes + round - 1) / round, 64, 1024 / std::max<int64_t>(positions, 1)});
         if (segments >= 4) p.segments = (int)segments;
     } else if (a.inner_stride == 1 && a.inner >= 16 && a.top <= 16 && (a.classes <= 1024 || positions >= 16384)) {
         p.kind = kMaps;
