@@ -297,8 +297,10 @@ inline __host__ __device__ int segment_floats(int top) { return 3 + 2 * top; }
 // `WAVES` waves of a workgroup take a row, or with several segments a row their part of it.  A wave loads 16 bytes a lane, U
 // times over before it uses them; rows may begin at any address: the scores in front of the first 16-byte boundary and
 // behind the last one are taken one by one.
+// bfloat16 is bound by its instructions too: two loads ahead and eight waves a SIMD, 127 us for 2047 rows of 131071 and 8
+// alternatives (537 MB), against 134 with four loads and five waves.  float32 takes four loads.
 template <int DT, int WAVES, int U>
-__global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void rows_kernel(const cbinfer_log_probs_args a, int64_t first_row, FastDiv inner, int segments, float *found)
+__global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64, DT == kBF16 ? 8 : 1) void rows_kernel(const cbinfer_log_probs_args a, int64_t first_row, FastDiv inner, int segments, float *found)
 {
     typedef typename Elem<DT>::type T;
     constexpr int V = Row<DT>::V, ROWS = WAVES < 4 ? 4 / WAVES : 1, NT = WAVES * 64;
@@ -651,7 +653,7 @@ Plan plan(const cbinfer_log_probs_args &a)
         // us a call, 4096 rows of 1000 bfloat16: a wave each 17, four waves each 32
         if (a.classes <= 2048) return p;
         p.waves = 4;
-        // Few long rows are cut into segments of one round of loads, up to 1024 workgroups, and joined by a second launch.
+        // Few long rows are cut into segments of one or two rounds of loads, up to 1024 workgroups, and joined by a second launch.
         // 64 rows of 100003 bfloat16: 29 us whole, 18 in segments, join included; one of 131071: 28 and 14.
         const int64_t round = 4 * 64 * 4 * (a.dtype == kF32 ? 4 : 8), segments = std::min<int64_t>({(a.classes + round - 1) / round, 64, 1024 / std::max<int64_t>(positions, 1)});
         if (segments >= 4) p.segments = (int)segments;
@@ -670,6 +672,7 @@ hipError_t run(hipStream_t st, const cbinfer_log_probs_args &a)
     const Plan p = plan(a);
     const int64_t positions = a.outer * a.inner;
     if (p.kind == kMaps) return p.waves == 4 ? map_any<DT, 4>(st, a) : map_any<DT, 1>(st, a);
+    constexpr int U = DT == kF32 ? 4 : 2;
     float *found = static_cast<float *>(a.workspace);
     const FastDiv inner = make_fastdiv((int)a.inner);
     const int per_block = p.kind == kRows && p.waves > 1 ? 1 : 4;
@@ -679,9 +682,9 @@ hipError_t run(hipStream_t st, const cbinfer_log_probs_args &a)
         if (p.kind != kRows)
             wave_kernel<DT><<<blocks, 256, 0, st>>>(a, first, inner);
         else if (p.waves == 1)
-            rows_kernel<DT, 1, 4><<<grid, 256, 0, st>>>(a, first, inner, p.segments, found);
+            rows_kernel<DT, 1, U><<<grid, 256, 0, st>>>(a, first, inner, p.segments, found);
         else
-            rows_kernel<DT, 4, 4><<<grid, 256, 0, st>>>(a, first, inner, p.segments, found);
+            rows_kernel<DT, 4, U><<<grid, 256, 0, st>>>(a, first, inner, p.segments, found);
         if (hipError_t e = hipGetLastError()) return e;
     }
     if (p.segments > 1) {
