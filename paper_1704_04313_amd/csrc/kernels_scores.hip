@@ -507,32 +507,100 @@ __global__ __launch_bounds__(256) void join_kernel(const cbinfer_log_probs_args 
 }
 
 // ---- positions behind one another: maps ------------------------------------------------------------
-// A lane takes a position and keeps its K best in registers, best first.
-template <int K>
-struct Ranked {
-    float v[K ? K : 1];
-    int i[K ? K : 1];
-    __device__ __forceinline__ void clear()
+// A lane takes a position and keeps its K best in registers, best first.  A score and its class are one key, so that the
+// larger and the smaller of two are one instruction each: CH classes are put in order by a network of such pairs, and joined with
+// the K so far by another.  Lanes differ in which scores are wanted, so nothing would be gained by asking.
+// bfloat16: 32 bits, 16 of the score and 16 of the class.  float32: 64 bits, 32 of the score and 31 of the class, as a
+// positive double: whatever a number's bits are, its exponent is not that of infinity, NaN or a denormal.
+template <int DT>
+struct Key;
+template <>
+struct Key<kBF16> {
+    unsigned k;
+    static __device__ __forceinline__ Key none() { return {0u}; }
+    static __device__ __forceinline__ Key of(float x, int c)
     {
-#pragma unroll
-        for (int j = 0; j < K; ++j) { v[j] = -__builtin_inff(); i[j] = kNone; }
+        const unsigned b = __float_as_uint(x + 0.0f); // -0 is 0
+        return {((b ^ ((unsigned)((int)b >> 31) | 0x80000000u)) & 0xffff0000u) | (0xffffu - (unsigned)c)};
     }
-    // NaN is never taken: rows that hold one are ranked again.
-    __device__ __forceinline__ void insert(float x, int c)
-    {
-#pragma unroll
-        for (int j = 0; j < K; ++j) {
-            const bool better = x > v[j] || (x == v[j] && c < i[j]);
-            const float ov = v[j];
-            const int oi = i[j];
-            v[j] = better ? x : ov;
-            i[j] = better ? c : oi;
-            x = better ? ov : x;
-            c = better ? oi : c;
-        }
-    }
-    __device__ __forceinline__ bool wants(float x) const { return K && (x > v[K ? K - 1 : 0] || i[K ? K - 1 : 0] == kNone); }
+    __device__ __forceinline__ int index() const { return (int)(0xffffu - (k & 0xffffu)); }
+    __device__ __forceinline__ float value() const { return __uint_as_float((k & 0x80000000u ? k ^ 0x80000000u : ~k) & 0xffff0000u); }
+    static __device__ __forceinline__ Key larger(Key a, Key b) { return {max(a.k, b.k)}; }
+    static __device__ __forceinline__ Key smaller(Key a, Key b) { return {min(a.k, b.k)}; }
+    static constexpr int kClasses = 1 << 16;
 };
+template <>
+struct Key<kF32> {
+    double k;
+    static __device__ __forceinline__ Key none() { return {0.0}; }
+    static __device__ __forceinline__ Key of(float x, int c)
+    {
+        const unsigned b = __float_as_uint(x + 0.0f), u = b ^ ((unsigned)((int)b >> 31) | 0x80000000u);
+        return {__hiloint2double((int)(u >> 1), (int)(u << 31 | (0x7fffffffu - (unsigned)c)))};
+    }
+    __device__ __forceinline__ int index() const { return (int)(0x7fffffffu - ((unsigned)__double2loint(k) & 0x7fffffffu)); }
+    __device__ __forceinline__ float value() const
+    {
+        const unsigned u = (unsigned)__double2hiint(k) << 1 | (unsigned)__double2loint(k) >> 31;
+        return of_key((int)(u ^ 0x80000000u));
+    }
+    // fmax and fmin would first make quiet NaNs of signalling ones; there are none
+    static __device__ __forceinline__ Key larger(Key a, Key b)
+    {
+        double r;
+        asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a.k), "v"(b.k));
+        return {r};
+    }
+    static __device__ __forceinline__ Key smaller(Key a, Key b)
+    {
+        double r;
+        asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a.k), "v"(b.k));
+        return {r};
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ void order(T &a, T &b)
+{
+    const T x = T::larger(a, b);
+    b = T::smaller(a, b);
+    a = x;
+}
+
+// Largest first.  A sequence that rises and falls (or the other way) is put in order by log2 N rounds of pairs.
+template <int N, typename T>
+__device__ __forceinline__ void order_bitonic(T (&x)[N])
+{
+#pragma unroll
+    for (int d = N / 2; d; d /= 2)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (!(i & d)) order(x[i], x[i + d]);
+}
+template <int N, typename T>
+__device__ __forceinline__ void order_all(T (&x)[N])
+{
+#pragma unroll
+    for (int n = 2; n <= N; n *= 2) {
+#pragma unroll
+        for (int i = 0; i < N; i += n) // two ordered halves: the first against the second turned round
+#pragma unroll
+            for (int j = 0; j < n / 2; ++j) order(x[i + j], x[i + n - 1 - j]);
+#pragma unroll
+        for (int d = n / 4; d; d /= 2)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (!(i & d)) order(x[i], x[i + d]);
+    }
+}
+// The N largest of both, in order.
+template <int N, typename T>
+__device__ __forceinline__ void order_join(T (&x)[N], const T (&y)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = T::larger(x[i], y[N - 1 - i]);
+    order_bitonic(x);
+}
 
 // careful_top for a lane by itself.
 template <int DT>
@@ -554,58 +622,75 @@ __device__ void careful_top_lane(const cbinfer_log_probs_args &a, int64_t base, 
 }
 
 // PARTS > 1: the waves of a workgroup share the classes of 256 / PARTS positions, for maps that would not fill the chip
-// otherwise.  CH classes are loaded before they are used.
+// otherwise.  CH classes are loaded while those before are worked on.
 template <int DT, int K, int PARTS>
 __global__ __launch_bounds__(256) void map_kernel(const cbinfer_log_probs_args a, FastDiv inner)
 {
-    constexpr int CH = 8, NP = 256 / PARTS;
     typedef typename Elem<DT>::type T;
-    __shared__ float sums[PARTS > 1 ? PARTS - 1 : 1][3 + 2 * K][PARTS > 1 ? NP : 1];
+    typedef Key<DT> Ranked;
+    constexpr int KK = K ? K : 1, CH = K > 8 ? K : 8, NP = 256 / PARTS;
+    __shared__ float sums[PARTS > 1 ? PARTS - 1 : 1][3][PARTS > 1 ? NP : 1];
+    __shared__ Ranked lists[PARTS > 1 ? PARTS - 1 : 1][KK][PARTS > 1 ? NP : 1];
     const int part = threadIdx.x / NP, place = threadIdx.x % NP;
     const int64_t pos = (int64_t)blockIdx.x * NP + place;
     const bool there = pos < a.outer * a.inner;
     const int o = there ? fast_div((int)pos, inner) : 0;
     const int64_t i = there ? pos - (int64_t)o * a.inner : 0, base = o * a.outer_stride + i * a.inner_stride;
-    const T *x = static_cast<const T *>(a.scores) + base;
     const Label label = there && part == 0 ? read_label<DT>(a, pos, base) : Label{-1, 0.0f};
     const int n = (int)a.classes, each = (n + PARTS - 1) / PARTS, end = min(n, (part + 1) * each);
+    const T *x = static_cast<const T *>(a.scores) + base + (int64_t)(part * each) * a.class_stride;
     Sums t = {kLowest, 0.0f, 0.0f};
-    Ranked<K> b;
-    b.clear();
-    if (there) {
-        for (int c0 = part * each; c0 < end; c0 += CH) {
-            float v[CH], most = kLowest;
+    Ranked best[KK];
 #pragma unroll
-            for (int e = 0; e < CH; ++e) {
-                v[e] = c0 + e < end ? Elem<DT>::get(x[(c0 + e) * a.class_stride]) : -__builtin_inff();
-                most = fmaxf(most, v[e]);
-            }
-            raise_to(t, fmaxf(t.m, most));
+    for (int j = 0; j < KK; ++j) best[j] = Ranked::none();
+    T next[CH];
+    const T none = Elem<DT>::put(-__builtin_inff());
+    auto load = [&](int c0) {
 #pragma unroll
-            for (int e = 0; e < CH; ++e) add(t, v[e]);
-            if (b.wants(most)) {
+        for (int e = 0; e < CH; ++e) next[e] = there && c0 + e < end ? x[e * a.class_stride] : none;
+        x += CH * a.class_stride;
+    };
+    load(part * each);
+    for (int c0 = part * each; c0 < end; c0 += CH) {
+        float v[CH], most = kLowest;
 #pragma unroll
-                for (int e = 0; e < CH; ++e)
-                    if (c0 + e < end && b.wants(v[e])) b.insert(v[e], c0 + e);
+        for (int e = 0; e < CH; ++e) {
+            v[e] = Elem<DT>::get(next[e]);
+            most = fmaxf(most, v[e]);
+        }
+        load(c0 + CH);
+        raise_to(t, fmaxf(t.m, most));
+#pragma unroll
+        for (int e = 0; e < CH; ++e) add(t, v[e]);
+        if constexpr (K == 1) {
+#pragma unroll
+            for (int e = 0; e < CH; ++e) best[0] = Ranked::larger(best[0], Ranked::of(v[e], c0 + e));
+        } else if constexpr (K > 1) {
+#pragma unroll
+            for (int g = 0; g < CH; g += KK) {
+                Ranked y[KK];
+#pragma unroll
+                for (int j = 0; j < KK; ++j) y[j] = Ranked::of(v[g + j], c0 + g + j);
+                order_all(y);
+                order_join(best, y);
             }
         }
     }
     if (PARTS > 1) {
         if (part) {
-            float (*mine)[PARTS > 1 ? NP : 1] = sums[part - 1];
-            mine[0][place] = t.m; mine[1][place] = t.s; mine[2][place] = t.t;
+            sums[part - 1][0][place] = t.m; sums[part - 1][1][place] = t.s; sums[part - 1][2][place] = t.t;
 #pragma unroll
-            for (int j = 0; j < K; ++j) { mine[3 + j][place] = b.v[j]; mine[3 + K + j][place] = __int_as_float(b.i[j]); }
+            for (int j = 0; j < K; ++j) lists[part - 1][j][place] = best[j];
         }
         __syncthreads();
         if (part) return;
-        for (int p = 0; p + 1 < PARTS; ++p) { // ascending classes
+        for (int p = 0; p + 1 < PARTS; ++p) {
             join(t, {sums[p][0][place], sums[p][1][place], sums[p][2][place]});
+            if constexpr (K > 0) {
+                Ranked y[KK];
 #pragma unroll
-            for (int j = 0; j < K; ++j) {
-                const float v = sums[p][3 + j][place];
-                const int c = __float_as_int(sums[p][3 + K + j][place]);
-                if (c != kNone && b.wants(v)) b.insert(v, c);
+                for (int j = 0; j < KK; ++j) y[j] = lists[p][j][place];
+                order_join(best, y);
             }
         }
     }
@@ -621,8 +706,8 @@ __global__ __launch_bounds__(256) void map_kernel(const cbinfer_log_probs_args a
 #pragma unroll
     for (int j = 0; j < K; ++j)
         if (j < a.top) {
-            a.top_values[to + j * a.inner] = log_prob(b.v[j], t, log_s);
-            a.top_index[to + j * a.inner] = b.i[j];
+            a.top_values[to + j * a.inner] = log_prob(best[j].value(), t, log_s);
+            a.top_index[to + j * a.inner] = best[j].index();
         }
 }
 
@@ -657,7 +742,8 @@ Plan plan(const cbinfer_log_probs_args &a)
         // 64 rows of 100003 bfloat16: 29 us whole, 18 in segments, join included; one of 131071: 28 and 14.
         const int64_t round = 4 * 64 * 4 * (a.dtype == kF32 ? 4 : 8), segments = std::min<int64_t>({(a.classes + round - 1) / round, 64, 1024 / std::max<int64_t>(positions, 1)});
         if (segments >= 4) p.segments = (int)segments;
-    } else if (a.inner_stride == 1 && a.inner >= 16 && a.top <= 16 && (a.classes <= 1024 || positions >= 16384)) {
+    } else if (a.inner_stride == 1 && a.inner >= 16 && a.top <= 16 && (a.classes <= 1024 || positions >= 16384) &&
+               (a.dtype == kF32 || a.classes <= Key<kBF16>::kClasses)) {
         p.kind = kMaps;
         p.waves = positions < 65536 && a.classes >= 32 ? 4 : 1;
     }
