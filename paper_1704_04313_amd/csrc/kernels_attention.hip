@@ -157,6 +157,12 @@ __device__ __forceinline__ f32x4 multiply(const u32x4 &a, const u32x4 &b, const 
 }
 __device__ __forceinline__ f32x4 multiply(float a, float b, const f32x4 &c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
+// Four bfloat16 of a column: 16 lanes give the addresses of four rows' four times four.
+__device__ __forceinline__ uint2 across_rows(const unsigned short *from)
+{
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)from));
+}
+
 // The upper halves of two words: the first in the lower half.
 __device__ __forceinline__ unsigned upper_halves(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
 __device__ __forceinline__ float cut(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
@@ -192,15 +198,25 @@ struct alignas(16) ChunkLds {
     // Rows are longer so that the lanes of an access reach different banks: 16 bytes where each lane reads 16 of a row of its own,
     // 64 where four rows are read across (bfloat16 K and V, transposed on the way).
     static constexpr int K = 32 * KT, V = 32 * NC, PAD = 16 / (int)sizeof(T), ACROSS = DT == kBF16 ? 32 : PAD;
-    static constexpr int KPAD = OUT ? PAD : ACROSS; // both ways where there are scores: 16 bytes are the better choice (49 us against 54)
+    static constexpr int KPAD = DT == kBF16 ? 0 : PAD; // bfloat16: see swizzle()
     T k[kChunk][K + KPAD], v[kChunk][V + ACROSS], q[OUT ? kChunk : 1][K + PAD];
     T p[DT == kBF16 ? 2 : 1][OUT ? kChunk : 1][kChunk + PAD]; // scores, by query; bfloat16: in two parts
     f32x4 other[OUT ? 2 * NC : 1][4][64]; // a wave's part of Q S for the queries of the wave beside it
-    float fade[kChunk];          // g^1 ... g^64
-    float fade_v[kChunk];        // g^(m-1) ... g^0 of the chunk at hand
-    float fade_back[2 * kChunk]; // g^63 ... g^0, then ones
+    float fade_v[kChunk];        // g^(m-1) ... g^0 of the chunk at hand, then ones
+    float fade_q[kChunk];        // scale g^1 ... scale g^64
+    float fade_back[2 * kChunk]; // scale g^63 ... scale g^0, then zeros
+    float fade[kChunk + 1];      // g^0 ... g^64
     int odd[2];                  // whether the chunk, and the next, hold a value that is not finite
 };
+
+// bfloat16 K is read along its rows for the scores (16 rows, 16 bytes of each) and across them for the state (four rows, 64
+// bytes of each): its pieces of 16 bytes change places within 256 bytes so that either takes 256 bytes from all the banks.  What
+// to exclusive-or a piece's number with.
+template <int KT>
+__device__ __forceinline__ int swizzle(int row)
+{
+    return KT == 2 ? (row & 2) << 1 | (row >> 2 & 3) : (row & 3) << 2 | (row >> 2 & 3);
+}
 
 // OUT: outputs of the tokens of a part (`per` chunks) of the sequence, from the state in front of it.  Otherwise what those
 // tokens leave in a state of zero, where further tokens follow.  `states`: [stream][head][part][key_size][value_size].
@@ -215,7 +231,7 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
     constexpr int KP = kChunk / KR, VP = kChunk / VR;
     static_assert(KR * KW == NT && VR * VW == NT && KP >= 1 && VP >= 1, "whole rows at a time");
     __shared__ Lds lds;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, side = lane & 31, half = lane >> 5, low = wave & 1, tile = wave >> 1;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), side = lane & 31, half = lane >> 5, low = (wave ^ wave >> 2) & 1, tile = wave >> 1;
     const int slice = blockIdx.x % slices, bh = blockIdx.x / slices, b = bh / a.heads, h = bh - b * a.heads, hk = h / (a.heads / a.kv_heads);
     const int part = blockIdx.y, dk = a.key_size, dv = a.value_size, column = slice * Lds::V + tile * 32 + side;
     const int n = a.lengths ? min(max(a.lengths[b], 0), a.tokens) : a.tokens;
@@ -273,9 +289,12 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
         const int i = threadIdx.x;
         const float f = power(g, i);
         lds.fade_v[kChunk - 1 - i] = f;
-        lds.fade_back[kChunk - 1 - i] = f;
-        lds.fade_back[kChunk + i] = 1.0f;
-        lds.fade[i] = power(g, i + 1);
+        lds.fade_back[kChunk - 1 - i] = a.scale * f;
+        lds.fade_back[kChunk + i] = 0.0f;
+        const float next = power(g, i + 1);
+        lds.fade_q[i] = a.scale * next;
+        lds.fade[i + 1] = next;
+        if (i == 0) lds.fade[0] = 1.0f;
     }
     if (threadIdx.x < 2) lds.odd[threadIdx.x] = 0;
     if (OUT) // scores of later keys in the tiles that are multiplied all the same
@@ -305,7 +324,8 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
         __syncthreads(); // the chunk before is done with LDS
 #pragma unroll
         for (int i = 0; i < KP; ++i) {
-            *reinterpret_cast<u32x4 *>(&lds.k[krow + i * KR][kcol]) = kr[i];
+            const int kat = DT == kBF16 ? 8 * (kcol / 8 ^ swizzle<KT>(krow + i * KR)) : kcol;
+            *reinterpret_cast<u32x4 *>(&lds.k[krow + i * KR][kat]) = kr[i];
             if (OUT) {
                 const u32x4 &x = qr[OUT ? i : 0];
                 if (DT == kBF16) { // of 16 values, groups of four in the order 0 2 1 3: as the accumulators have S
@@ -338,9 +358,26 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
             }
             if (odd) lds.odd[turn] = 1;
         }
-        if (m < kChunk && threadIdx.x < kChunk) lds.fade_v[threadIdx.x] = lds.fade_back[min((int)threadIdx.x + kChunk - m, kChunk - 1)];
+        if (m < kChunk && threadIdx.x < kChunk) lds.fade_v[threadIdx.x] = lds.fade[max(m - 1 - (int)threadIdx.x, 0)];
         __syncthreads();
         if (t + kChunk < t1) load(t1 - t - kChunk);
+
+        // The wave's columns of V as the second operand of a product: bfloat16 of 16 tokens from 16 s on, 8 for either half of the lanes;
+        // float32 of 8 from 8 c on, 4 for either.
+        u32x4 vs[DT == kBF16 ? 4 : 8];
+        if constexpr (DT == kBF16) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const T *from = &lds.v[16 * s + 8 * half + (lane & 15) / 4][tile * 32 + (lane & 16) + 4 * (lane & 3)];
+                const uint2 x = across_rows(from), y = across_rows(from + 4 * (Lds::V + Lds::ACROSS));
+                vs[s] = u32x4{x.x, x.y, y.x, y.y};
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) vs[c][e] = __float_as_uint(Elem<DT>::get(lds.v[8 * c + 4 * half + e][tile * 32 + side]));
+        }
 
         f32x16 acc;
         if (OUT) {
@@ -350,10 +387,11 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
                 const int it = at < 1 ? 0 : at < 3 ? 1 : at < 6 ? 2 : 3, j0 = 16 * (at - it * (it + 1) / 2), col = lane & 15, quarter = lane >> 4;
                 f32x4 p = {0, 0, 0, 0};
                 if constexpr (DT == kBF16) {
-                    const T *kp = &lds.k[j0 + col][16 * (quarter >> 1) + 4 * (quarter & 1)], *qp = &lds.q[16 * it + col][8 * quarter];
+                    const T *kp = &lds.k[j0 + col][4 * (quarter & 1)], *qp = &lds.q[16 * it + col][8 * quarter];
+                    const int piece = 2 * (quarter >> 1) ^ swizzle<KT>(col);
 #pragma unroll 4
                     for (int s = 0; s < KT; ++s) {
-                        const uint2 x = *reinterpret_cast<const uint2 *>(kp + 32 * s), y = *reinterpret_cast<const uint2 *>(kp + 32 * s + 8);
+                        const uint2 x = *reinterpret_cast<const uint2 *>(kp + 8 * (4 * s ^ piece)), y = *reinterpret_cast<const uint2 *>(kp + 8 * (4 * s + 1 ^ piece));
                         p = multiply(u32x4{x.x, x.y, y.x, y.y}, *reinterpret_cast<const u32x4 *>(qp + 32 * s), p);
                     }
                 } else {
@@ -378,7 +416,8 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
                 }
             }
             // this wave's rows of S in Q S
-            f32x16 qs[2] = {};
+            f32x16 qs[2] = {}; // for the queries that are its own, and for the other wave's
+            const int across = 32 * (low ? -1 : 1) * (Lds::K + Lds::PAD);
 #pragma unroll
             for (int kt = 0; kt < KH; ++kt) {
                 if constexpr (DT == kBF16) {
@@ -389,8 +428,8 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
 #pragma unroll
                         for (int e = 0; e < 8; ++e) x[e] = S[kt][8 * s + e];
                         split(x, y);
-                        const T *qp = &lds.q[side][32 * (KH * low + kt) + 16 * s + 8 * half];
-                        const u32x4 z0 = *reinterpret_cast<const u32x4 *>(qp), z1 = *reinterpret_cast<const u32x4 *>(qp + 32 * (Lds::K + Lds::PAD));
+                        const T *qp = &lds.q[32 * low + side][32 * (KH * low + kt) + 16 * s + 8 * half];
+                        const u32x4 z0 = *reinterpret_cast<const u32x4 *>(qp), z1 = *reinterpret_cast<const u32x4 *>(qp + across);
                         qs[0] = multiply(z0, y[0], qs[0]);
                         qs[1] = multiply(z1, y[0], qs[1]);
                         qs[0] = multiply(z0, y[1], qs[0]);
@@ -399,8 +438,8 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
                 } else {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const T *qp = &lds.q[side][32 * (KH * low + kt) + 8 * c + 4 * half];
-                        const f32x4 z0 = *reinterpret_cast<const f32x4 *>(qp), z1 = *reinterpret_cast<const f32x4 *>(qp + 32 * (Lds::K + Lds::PAD));
+                        const T *qp = &lds.q[32 * low + side][32 * (KH * low + kt) + 8 * c + 4 * half];
+                        const f32x4 z0 = *reinterpret_cast<const f32x4 *>(qp), z1 = *reinterpret_cast<const f32x4 *>(qp + across);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             qs[0] = multiply(z0[e], S[kt][4 * c + e], qs[0]);
@@ -409,65 +448,73 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
                     }
                 }
             }
+            acc = qs[0];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[r] = low ? qs[1][r] : qs[0][r];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                f32x4 x;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = low ? qs[0][4 * c + e] : qs[1][4 * c + e];
-                lds.other[wave ^ 1][c][lane] = x;
-            }
+            for (int c = 0; c < 4; ++c) lds.other[wave ^ 1][c][lane] = f32x4{qs[1][4 * c], qs[1][4 * c + 1], qs[1][4 * c + 2], qs[1][4 * c + 3]};
         }
 
-        // the wave's columns of V as the second operand: bfloat16 of 16 tokens from 16 s on, by the lane half; float32 of 8 from 8 c on
-        auto v16 = [&](int s) {
+        // the state behind the chunk
+        const float all = lds.fade[m];
+#pragma unroll
+        for (int kt = 0; kt < KH; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) S[kt][r] *= all;
+        if constexpr (DT == kBF16) {
             const int in = lane & 15;
-            const T *from = &lds.v[16 * s + 8 * half + in / 4][tile * 32 + (lane & 16) + 4 * (in & 3)];
-            const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)from));
-            const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(from + 4 * (Lds::V + Lds::ACROSS))));
-            return u32x4{x.x, x.y, y.x, y.y};
-        };
-        auto v8 = [&](int c) {
-            f32x4 x;
+#pragma unroll 4
+            for (int s = 0; s < 4; ++s) {
+                const f32x4 f0 = *reinterpret_cast<const f32x4 *>(&lds.fade_v[16 * s + 8 * half]), f1 = *reinterpret_cast<const f32x4 *>(&lds.fade_v[16 * s + 8 * half + 4]);
+                float x[8];
+                u32x4 y[3];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = Elem<DT>::get(lds.v[8 * c + 4 * half + e][tile * 32 + side]);
-            return x;
-        };
-
-        // 16 tokens of V as they fade up to the chunk's end, in three parts
-        auto fading = [&](int s, u32x4 (&y)[3]) {
-            const f32x4 f0 = *reinterpret_cast<const f32x4 *>(&lds.fade_v[16 * s + 8 * half]), f1 = *reinterpret_cast<const f32x4 *>(&lds.fade_v[16 * s + 8 * half + 4]);
-            const u32x4 vb = v16(s);
-            float x[8];
+                for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(e & 1 ? vs[s][e / 2] & 0xffff0000u : vs[s][e / 2] << 16) * (e < 4 ? f0[e % 4] : f1[e % 4]);
+                split(x, y);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(e & 1 ? vb[e / 2] & 0xffff0000u : vb[e / 2] << 16) * (e < 4 ? f0[e % 4] : f1[e % 4]);
-            split(x, y);
-        };
+                for (int kt = 0; kt < KH; ++kt) {
+                    const int row = 8 * half + in / 4, piece = 4 * (KH * low + kt) + (lane >> 3 & 2) + (in >> 1 & 1);
+                    const T *from = &lds.k[16 * s + row][8 * (piece ^ swizzle<KT>(row)) + 4 * (in & 1)];
+                    const T *next = &lds.k[16 * s + row + 4][8 * (piece ^ swizzle<KT>(row + 4)) + 4 * (in & 1)];
+                    const uint2 p = across_rows(from), u = across_rows(next);
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) S[kt] = multiply(u32x4{p.x, p.y, u.x, u.y}, y[i], S[kt]);
+                }
+            }
+        } else {
+#pragma unroll 4
+            for (int c = 0; c < 8; ++c) {
+                const f32x4 f = *reinterpret_cast<const f32x4 *>(&lds.fade_v[8 * c + 4 * half]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x = __uint_as_float(vs[DT == kBF16 ? 0 : c][e]) * f[e];
+#pragma unroll
+                    for (int kt = 0; kt < KH; ++kt) S[kt] = multiply(lds.k[8 * c + 4 * half + e][32 * (KH * low + kt) + side], x, S[kt]);
+                }
+            }
+        }
         if (OUT) {
             __syncthreads(); // the scores are there, and the other wave's part
             const int i0 = 32 * low + 4 * half; // of register r: query i0 + 8 (r / 4) + r % 4
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                const f32x4 x = lds.other[wave][c][lane], f = *reinterpret_cast<const f32x4 *>(&lds.fade[i0 + 8 * c]);
+                const f32x4 x = lds.other[wave][c][lane], f = *reinterpret_cast<const f32x4 *>(&lds.fade_q[i0 + 8 * c]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[4 * c + e] = (acc[4 * c + e] + x[e]) * f[e];
             }
             if (!lds.odd[turn]) {
                 if constexpr (DT == kBF16) {
-#pragma unroll 2
-                    for (int s = 0; s < 2 + 2 * low; ++s) {
-                        const u32x4 y = v16(s);
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) acc = multiply(*reinterpret_cast<const u32x4 *>(&lds.p[DT == kBF16 ? i : 0][32 * low + side][16 * s + 8 * half]), y, acc);
-                    }
+                    for (int s = 0; s < 4; ++s)
+                        if (s < 2 + 2 * low)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) acc = multiply(*reinterpret_cast<const u32x4 *>(&lds.p[DT == kBF16 ? i : 0][32 * low + side][16 * s + 8 * half]), vs[s], acc);
                 } else {
-#pragma unroll 2
-                    for (int c = 0; c < 4 + 4 * low; ++c) {
-                        const f32x4 z = *reinterpret_cast<const f32x4 *>(&lds.p[0][32 * low + side][8 * c + 4 * half]), y = v8(c);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc = multiply(z[e], y[e], acc);
-                    }
+                    for (int c = 0; c < 8; ++c)
+                        if (c < 4 + 4 * low) {
+                            const f32x4 z = *reinterpret_cast<const f32x4 *>(&lds.p[0][32 * low + side][8 * c + 4 * half]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc = multiply(z[e], __uint_as_float(vs[c % (DT == kBF16 ? 4 : 8)][e]), acc);
+                        }
                 }
             } else { // a value that is not finite: its product with the score 0 of an earlier token must not be added
                 for (int j = 0; j < m; ++j) {
@@ -490,49 +537,15 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
                 for (int r = 0; r < 16; ++r) {
                     const unsigned at = from + (8 * (r / 4) + r % 4) * each;
                     if constexpr (DT == kBF16)
-                        __builtin_amdgcn_raw_buffer_store_b16(Elem<DT>::put(a.scale * acc[r]), to, at, 0, 0);
+                        __builtin_amdgcn_raw_buffer_store_b16(Elem<DT>::put(acc[r]), to, at, 0, 0);
                     else
-                        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(a.scale * acc[r]), to, at, 0, 0);
+                        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(acc[r]), to, at, 0, 0);
                 }
             } else {
                 T *to = o + (int64_t)(t + i0) * a.o_stride[1] + column;
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (i0 + 8 * (r / 4) + r % 4 < m && column < dv) to[(8 * (r / 4) + r % 4) * a.o_stride[1]] = Elem<DT>::put(a.scale * acc[r]);
-            }
-        }
-
-        // the state behind the chunk
-        const float all = lds.fade[m - 1];
-#pragma unroll
-        for (int kt = 0; kt < KH; ++kt)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) S[kt][r] *= all;
-        if constexpr (DT == kBF16) {
-            const int in = lane & 15;
-#pragma unroll 4
-            for (int s = 0; s < 4; ++s) {
-                u32x4 y[3];
-                fading(s, y);
-#pragma unroll
-                for (int kt = 0; kt < KH; ++kt) {
-                    const T *from = &lds.k[16 * s + 8 * half + in / 4][32 * (KH * low + kt) + (lane & 16) + 4 * (in & 3)];
-                    const uint2 p = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)from));
-                    const uint2 u = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(from + 4 * (Lds::K + Lds::KPAD))));
-#pragma unroll
-                    for (int i = 0; i < 3; ++i) S[kt] = multiply(u32x4{p.x, p.y, u.x, u.y}, y[i], S[kt]);
-                }
-            }
-        } else {
-#pragma unroll 4
-            for (int c = 0; c < 8; ++c) {
-                const f32x4 f = *reinterpret_cast<const f32x4 *>(&lds.fade_v[8 * c + 4 * half]), y = v8(c);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = y[e] * f[e];
-#pragma unroll
-                    for (int kt = 0; kt < KH; ++kt) S[kt] = multiply(lds.k[8 * c + 4 * half + e][32 * (KH * low + kt) + side], x, S[kt]);
-                }
+                    if (i0 + 8 * (r / 4) + r % 4 < m && column < dv) to[(8 * (r / 4) + r % 4) * a.o_stride[1]] = Elem<DT>::put(acc[r]);
             }
         }
     }
@@ -583,9 +596,9 @@ Plan plan(const cbinfer_linear_attention_args &a)
     p.slices = (tiles + p.tiles - 1) / p.tiles;
     const int64_t groups = (int64_t)a.streams * a.heads * p.slices, chunks = (a.tokens + kChunk - 1) / kChunk;
     // Parts until every compute unit has a workgroup; their keys and values are read twice.  us for 8192 tokens, 16 heads of 128: 8 parts 119,
-    // 16 78, 32 93.  Streams of different lengths leave compute units idle: twice as many (12 streams of up to 1023 tokens, 6 heads,
-    // float32: 3 parts 83, 7 70).
-    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(chunks / 2, (a.lengths ? 512 : 256) / std::max<int64_t>(groups, 1)));
+    // 16 78, 32 93.  Streams of different lengths leave compute units idle: two and a half times as many (12 streams of up to 1023 tokens,
+    // 6 heads, float32: 3 parts 83, 6 69, 8 62, 16 66).
+    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(chunks / 2, (a.lengths ? 640 : 256) / std::max<int64_t>(groups, 1)));
     p.per = (int)((chunks + p.parts - 1) / p.parts);
     p.parts = (int)((chunks + p.per - 1) / p.per);
     return p;
