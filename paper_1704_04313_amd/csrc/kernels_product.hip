@@ -331,14 +331,21 @@ auto with_shape(const cbinfer_quantised_product_args &a, F f)
             // 4 tokens, 4729 x 20806: parts of 16 blocks 26.8, of 32 27.3
             return f(Shape<DT, 1, 2, 2, 8, 2>());
         }
-        // 64 tokens, 100003 x 2048: four tiles of tokens at a time 62, two (the weights pass twice) 97; 4096 x 4096: 17.6, 15.3
+        // 64 tokens, 100003 x 2048: four tiles of tokens at a time 62, two of 16 waves 80
         if (a.tokens > 32 && tiles >= 1024) return f(Shape<DT, 4, 2, 2, 8, 1>());
-        return f(Shape<DT, 2, 2, 2, 8, 1>());
+        // 64 tokens, 4096 x 4096: 16 waves and a tile at a time, which take rows whole, 11.3, two tiles in two parts 13.7, of 8 waves 14.5
+        // (24 tokens, 50000 x 4096: 53, as the weights pass twice, and two tiles 48)
+        if (blocks > 16 && blocks <= 32 && tiles < 1024) return f(Shape<DT, 1, 2, 2, 16, 1>());
+        if (blocks > 16 && blocks <= 32) return f(Shape<DT, 2, 2, 2, 8, 1>());
+        // 64 tokens, 8192 x 2048: 10.2, one tile at a time 16.7, 8 waves 10.9; 256 x 38400: 14.7, 16.1, 16.9
+        return f(Shape<DT, 2, 1, 2, 16, 1>());
     } else {
         // three parts of x take three times the registers.  16 tokens, 36122 x 5669: 48.9, with 16 waves 50.8
         if (a.tokens <= 16) return f(Shape<DT, 1, 1, 4, 8, 2>());
-        // 64 tokens, 256 x 38400: two tiles at a time 20.8, four 29; 8192 x 2048: 20.8, 28.6
-        return f(Shape<DT, 2, 1, 2, 8, 1>());
+        // 64 tokens, 256 x 38400: 18.9, 8 waves and two tiles of tokens at a time 21.2; four tiles of rows at a time 20.4, but 64 tokens,
+        // 8192 x 2048: 14.1 against 15.8
+        if (tiles < 64) return f(Shape<DT, 1, 1, 2, 16, 1>());
+        return f(Shape<DT, 1, 1, 4, 16, 1>());
     }
 }
 

@@ -78,7 +78,7 @@ int check(const cbinfer_quantised_product_args *a)
     if (!a) return refuse(CBINFER_EINVAL, "%s: arguments are NULL", w);
     if (!known(a->dtype)) return refuse(CBINFER_EINVAL, "%s: dtype must be CBINFER_F32 or CBINFER_BF16", w);
     if (cbinfer_packed_weights_bytes(a->rows, a->cols, a->group) == 0) return CBINFER_EINVAL;
-    if (a->tokens < 0 || a->tokens > (1 << 20)) return refuse(CBINFER_EUNSUPPORTED, "%s: tokens must be 0 .. 2^20", w);
+    if (a->tokens < 0 || a->tokens > (1 << 19)) return refuse(CBINFER_EUNSUPPORTED, "%s: tokens must be 0 .. 2^19", w);
     return CBINFER_OK;
 }
 
@@ -146,8 +146,8 @@ int cbinfer_quantise_weights(const void *weights, int32_t dtype, int64_t rows, i
 size_t cbinfer_packed_weights_bytes(int64_t rows, int64_t cols, int32_t group)
 {
     // threads of a launch are counted in 32 bits
-    if (rows < 1 || cols < 1 || rows > (1 << 26) || cols > (1 << 26) || rows * cols > (int64_t)1 << 32) {
-        refuse(CBINFER_EINVAL, "4-bit weights: rows and cols must be 1 .. 2^26, together at most 2^32");
+    if (rows < 1 || cols < 1 || rows > (1 << 26) || cols > (1 << 25) || rows * cols > (int64_t)1 << 32) {
+        refuse(CBINFER_EINVAL, "4-bit weights: rows and cols must be 1 .. 2^26 and 1 .. 2^25, together at most 2^32");
         return 0;
     }
     if (group != 32 && group != 64 && group != 128) {

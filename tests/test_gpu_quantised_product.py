@@ -146,3 +146,24 @@ def test_ties_take_the_even_code():
     codes, scales = cb.quantise_weights(w.cuda(), 32)
     assert float(scales) == 1.0
     assert codes[0, :16].tolist() == [0, 2, 2, 4, 4, 6, 6, 7, 0, 10, 10, 12, 12, 14, 14, 15]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k,group", [(20, 16400, 2100, 64), (40, 16401, 140, 32), (24, 1030, 2900, 128), (50, 1500, 900, 64)])
+def test_many_rows(m, n, k, group, dtype):
+    codes, scales, bias, layer = _layer(n, k, group, m + n)
+    x = torch.randn(m, k, generator=torch.Generator().manual_seed(2)).to(dtype).cuda()
+    _check(layer(x), x, codes, scales, bias, group, "%dx%dx%d" % (m, n, k))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_as_many_tokens_and_as_long_a_row_as_there_may_be(dtype):
+    codes, scales, bias, layer = _layer(3, 2, 32, 5)
+    x = torch.randn(1 << 19, 2, generator=torch.Generator().manual_seed(3)).to(dtype).cuda()
+    _check(layer(x), x, codes, scales, bias, 32, "2^19 tokens")
+    codes = torch.full((1, 1 << 25), 2, dtype=torch.uint8, device="cuda")  # ones
+    layer = cb.QuantisedLinear(codes, torch.ones(1, 1 << 18, dtype=torch.bfloat16, device="cuda"), group=128)
+    x = torch.zeros(1, 1 << 25, dtype=dtype, device="cuda")
+    for at, value in ((0, 1.0), (1023, 2.0), (1024, 4.0), ((1 << 24) + 1, 8.0), ((1 << 25) - 1, 16.0)):
+        x[0, at] = value
+    assert layer(x).item() == 31.0

@@ -109,6 +109,14 @@ def test_packed_weights_take_half_a_byte_and_their_scales():
         assert lib.cbinfer_packed_weights_bytes(rows, cols, group) == 0
 
 
+def test_limits_of_a_launch():
+    """A launch has 65535 groups of 16 tokens, and as many parts of 1024 columns, at most."""
+    lib = tokens._library()
+    assert lib.cbinfer_packed_weights_bytes(1, 1 << 25, 64) and not lib.cbinfer_packed_weights_bytes(1, (1 << 25) + 1, 64)
+    a = tokens.quantised_product_args(dtype=0, group=64, tokens=1, rows=8, cols=8, x_stride=8, y_stride=8, x=256, packed=256, y=256)
+    _bad("cbinfer_quantised_product", a, dict(tokens=(1 << 19) + 1), "2^19")
+
+
 def test_tensors_on_the_cpu_are_refused():
     x = torch.zeros(4, 8)
     for call in (lambda: cb.log_probs(x), lambda: cb.gated_norm(x), lambda: cb.quantise_weights(x),
