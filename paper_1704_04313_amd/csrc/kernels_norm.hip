@@ -29,7 +29,8 @@ __device__ __forceinline__ float gate_of(float g, int kind)
     return kind == CBINFER_GATE_SIGMOID ? open : g * open;
 }
 
-// Any size, group, stride and alignment: the row lies in LDS as float32.
+// Any size, group, stride and alignment: the row lies in LDS as float32.  One value a thread and load: 8192 rows of 4095 bfloat16
+// with a gate 86 us, where rows of 4096 take 38 in the kernel below.
 template <int DT, int DS>
 __global__ __launch_bounds__(256) void norm_row_kernel(const cbinfer_gated_norm_args a, int64_t first)
 {

@@ -31,6 +31,15 @@ __device__ __forceinline__ bf16x8 values_of(unsigned w)
 }
 
 // ---- laying out ----------------------------------------------------------------------------------
+__device__ __forceinline__ unsigned four_codes(unsigned x) // of four bytes, in the lower half
+{
+    x &= 0x0f0f0f0fu;
+    x = (x | x >> 4) & 0x00ff00ffu;
+    return (x | x >> 8) & 0xffffu;
+}
+
+// Once a layer.  WHOLE: eight codes at 8-byte addresses at a time, 100003 x 2048 76 us (308 MB); one by one 100003 x 2047 314.
+template <bool WHOLE>
 __global__ __launch_bounds__(256) void pack_codes_kernel(const uint8_t *codes, int64_t rows, int64_t cols, int64_t blocks, int64_t units, uint4 *to)
 {
     const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; // 16 bytes: a lane's part of a block
@@ -41,9 +50,15 @@ __global__ __launch_bounds__(256) void pack_codes_kernel(const uint8_t *codes, i
     unsigned w[4];
     for (int j = 0; j < 4; ++j) {
         w[j] = 0;
-        for (int e = 0; e < 8; ++e) {
-            const int64_t k = k0 + j * 32 + e;
-            if (n < rows && k < cols) w[j] |= (unsigned)(codes[n * cols + k] & 15) << (4 * e);
+        const int64_t k = k0 + j * 32;
+        if (n >= rows) continue;
+        if (WHOLE) {
+            if (k >= cols) continue;
+            const uint2 x = *reinterpret_cast<const uint2 *>(codes + n * cols + k);
+            w[j] = four_codes(x.x) | four_codes(x.y) << 16;
+        } else {
+            for (int e = 0; e < 8; ++e)
+                if (k + e < cols) w[j] |= (unsigned)(codes[n * cols + k + e] & 15) << (4 * e);
         }
     }
     to[u] = make_uint4(w[0], w[1], w[2], w[3]);
@@ -59,7 +74,7 @@ __global__ __launch_bounds__(256) void pack_scales_kernel(const uint16_t *scales
     to[u] = n < rows && k < groups ? scales[n * groups + k] : (uint16_t)0;
 }
 
-// 32 lanes a group.
+// 32 lanes a group; 100003 x 2048 float32 436 us.
 template <int DT>
 __global__ __launch_bounds__(256) void quantise_kernel(const typename Elem<DT>::type *w, int64_t rows, int64_t cols, int64_t stride, int group, int64_t groups, uint8_t *codes, uint16_t *scales)
 {
@@ -372,7 +387,8 @@ hipError_t pack_weights(hipStream_t st, const uint8_t *codes, const uint16_t *sc
                         void *packed)
 {
     const int64_t blocks = blocks_of(cols), units = tiles_of(rows) * blocks * 64, per_block = 128 / group, total = units / 4 * per_block;
-    pack_codes_kernel<<<(unsigned)((units + 255) / 256), 256, 0, st>>>(codes, rows, cols, blocks, units, static_cast<uint4 *>(packed));
+    const auto pack = cols % 8 == 0 && reinterpret_cast<uintptr_t>(codes) % 8 == 0 ? pack_codes_kernel<true> : pack_codes_kernel<false>;
+    pack<<<(unsigned)((units + 255) / 256), 256, 0, st>>>(codes, rows, cols, blocks, units, static_cast<uint4 *>(packed));
     if (hipError_t e = hipGetLastError()) return e;
     pack_scales_kernel<<<(unsigned)((total + 255) / 256), 256, 0, st>>>(scales, rows, (cols + group - 1) / group, blocks, (int)per_block, total,
         reinterpret_cast<uint16_t *>(static_cast<char *>(packed) + code_bytes(rows, cols)));
