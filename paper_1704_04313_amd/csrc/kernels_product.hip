@@ -256,25 +256,26 @@ __global__ __launch_bounds__(WAVES * 64, WAVES * PER_CU / 4) void product_kernel
 #pragma unroll
             for (int m = 0; m < MT; ++m) sums[turn][wave][r * MT + m][lane] = acc[r][m];
         __syncthreads(); // the other turn's sums were read before this
-        for (int at = wave; at < R * MT; at += WAVES) {
-            f32x4 y = sums[turn][0][at][lane];
-#pragma unroll 4 // more at a time would cost registers that hold x
-            for (int w = 1; w < WAVES; ++w) {
-                const f32x4 z = sums[turn][w][at][lane];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] += z[e];
-            }
-            const int r = at / MT, m = at - r * MT;
-            const int64_t n = ((int64_t)group * R + r) * 16 + (lane & 15), t = token0 + 16 * m + (lane >> 4) * 4;
-            if (n >= a.rows) continue;
+        // every wave its share, V values a lane: a few waves alone would hold the others up (24 tokens, 100003 x 2048: 47 us, so 32)
+        constexpr int V = R * MT % WAVES == 0 ? 4 : 2 * R * MT % WAVES == 0 ? 2 : 1, AHEAD = V == 4 ? 4 : 8; // more would cost registers that hold x
+        typedef float Values __attribute__((ext_vector_type(V)));
+        for (int at = threadIdx.x; at < R * MT * 256 / V; at += WAVES * 64) {
+            const int tile = at / (256 / V), r = tile / MT, m = tile - r * MT, l = at / (4 / V) & 63;
+            const int64_t n = ((int64_t)group * R + r) * 16 + (l & 15), t = token0 + 16 * m + (l >> 4) * 4 + at % (4 / V) * V;
+            if (n >= a.rows || t >= a.tokens) continue;
+            const Values *z = reinterpret_cast<const Values *>(&sums[turn][0][0][0]) + at;
+            Values y = z[0];
+#pragma unroll AHEAD
+            for (int w = 1; w < WAVES; ++w) y += z[w * (R * MT * 256 / V)];
             const float bias = a.bias && !partial ? a.bias[n] : 0.0f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < V; ++e)
                 if (t + e < a.tokens) {
+                    const float v = y[e];
                     if (partial)
-                        partial[((int64_t)blockIdx.y * a.tokens + t + e) * a.rows + n] = y[e];
+                        partial[((int64_t)blockIdx.y * a.tokens + t + e) * a.rows + n] = v;
                     else
-                        static_cast<T *>(a.y)[(t + e) * a.y_stride + n] = Elem<DT>::put(y[e] + bias);
+                        static_cast<T *>(a.y)[(t + e) * a.y_stride + n] = Elem<DT>::put(v + bias);
                 }
         }
     }
@@ -335,32 +336,37 @@ auto with_shape(const cbinfer_quantised_product_args &a, F f)
     if constexpr (DT == kBF16) {
         if (a.tokens <= 16) {
             if (blocks <= 8) return f(Shape<DT, 1, 1, 4, 8, 2>());
-            // us for 100003 x 2048 (115 MB) and 16 tokens: R = 3 33.5, 2 36.0, 4 (registers spill) 35.7; 16 waves, half of them without a block, 55
-            if (blocks <= 16) return f(Shape<DT, 1, 2, 3, 8, 2>());
-            if (blocks <= 32) {
-                // one token, 4096 x 4096: a row's tiles one by one 9.2, in two parts of 8 waves 14
+            if (blocks > 16 && blocks <= 32) {
+                // 1 token, 4096 x 4096: a row's tiles one by one 7.3, in two parts of 8 waves 14; 20000 x 4096: 11.1, two at a time 11.7
                 if (tiles <= 512) return f(Shape<DT, 1, 2, 1, 16, 1>());
-                // 16 tokens, 100003 x 4096: 48.8, in two parts 50.3
+                // 16 tokens, 100003 x 4096: 46.7, tiles one by one 57.7
                 return f(Shape<DT, 1, 2, 2, 16, 1>());
             }
-            // 4 tokens, 4729 x 20806: parts of 16 blocks 26.8, of 32 27.3
-            return f(Shape<DT, 1, 2, 2, 8, 2>());
+            // 16 tokens, 100003 x 2048 (115 MB): 29.8, four tiles at a time 31.5, two 48, of 8 waves with two blocks each 32.6; 4 tokens,
+            // 4729 x 20806: 19.7, parts of 32 blocks 23.7
+            return f(Shape<DT, 1, 1, 3, 16, 1>());
         }
-        // 64 tokens, 100003 x 2048: four tiles of tokens at a time 62, two of 16 waves 80
+        // 17 tokens, 40000 x 1000: 14.1, of 16 waves, half of them without a block, 18.2
+        if (blocks <= 8) return f(Shape<DT, 2, 1, 2, 8, 2>());
+        // 64 tokens, 100003 x 2048: four tiles of tokens at a time 69, two of 16 waves 83
         if (a.tokens > 32 && tiles >= 1024) return f(Shape<DT, 4, 2, 2, 8, 1>());
-        // 64 tokens, 4096 x 4096: 16 waves and a tile at a time, which take rows whole, 11.3, two tiles in two parts 13.7, of 8 waves 14.5
-        // (24 tokens, 50000 x 4096: 53, as the weights pass twice, and two tiles 48)
+        // 64 tokens, 4096 x 4096: 16 waves and a tile at a time, which take rows whole, 10.2, two tiles in two parts 13.7, of 8 waves 14.5
+        // (24 tokens, 50000 x 4096: 53, as the weights pass twice, and two tiles 43)
         if (blocks > 16 && blocks <= 32 && tiles < 1024) return f(Shape<DT, 1, 2, 2, 16, 1>());
         if (blocks > 16 && blocks <= 32) return f(Shape<DT, 2, 2, 2, 8, 1>());
-        // 64 tokens, 8192 x 2048: 10.2, one tile at a time 16.7, 8 waves 10.9; 256 x 38400: 14.7, 16.1, 16.9
+        // 64 tokens, 8192 x 2048: 9.4, one tile at a time 16.7, 8 waves 10.9; 256 x 38400: 14.1, 16.1, 16.9
         return f(Shape<DT, 2, 1, 2, 16, 1>());
     } else {
-        // three parts of x take three times the registers.  16 tokens, 36122 x 5669: 48.9, with 16 waves 50.8
-        if (a.tokens <= 16) return f(Shape<DT, 1, 1, 4, 8, 2>());
-        // 64 tokens, 256 x 38400: 18.9, 8 waves and two tiles of tokens at a time 21.2; four tiles of rows at a time 20.4, but 64 tokens,
-        // 8192 x 2048: 14.1 against 15.8
-        if (tiles < 64) return f(Shape<DT, 1, 1, 2, 16, 1>());
-        return f(Shape<DT, 1, 1, 4, 16, 1>());
+        // three parts of x take three times the registers
+        if (a.tokens <= 16 && blocks <= 8) return f(Shape<DT, 1, 1, 4, 8, 2>());
+        // 17 tokens, 40000 x 1000: 16, of 16 waves 25
+        if (blocks <= 8) return f(Shape<DT, 1, 1, 2, 8, 2>());
+        // 16 tokens, 100003 x 2048: 30.7, of 8 waves 40.6; 36122 x 5669: 44.6, 46.1.  64 tokens, 256 x 38400: 17.7, 8 waves and two tiles of
+        // tokens at a time 21.2, four tiles of rows 20.4
+        if (a.tokens <= 16 || tiles < 64) return f(Shape<DT, 1, 1, 2, 16, 1>());
+        // 64 tokens, 8192 x 2048: 12.7, three tiles at a time 14.3; 100003 x 2048: 113, 103
+        if (tiles < 1024) return f(Shape<DT, 1, 1, 4, 16, 1>());
+        return f(Shape<DT, 1, 1, 3, 16, 1>());
     }
 }
 
