@@ -105,15 +105,16 @@ __global__ __launch_bounds__(256) void quantise_kernel(const typename Elem<DT>::
 // Eight values of a token from column k on as they lie in memory, zeros beyond the row.
 template <int DT>
 struct Eight {
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4), aligned(2))); // one load at any alignment
     static constexpr int N = DT == kF32 ? 2 : 1;
     uint4 u[N];
-    // at a 16-byte address; the address is valid also where the token is not there
+    // at any address; it is valid also where the token is not there
     __device__ __forceinline__ void load(const typename Elem<DT>::type *x, bool there)
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            u[i] = reinterpret_cast<const uint4 *>(x)[i];
-            if (!there) u[i] = make_uint4(0, 0, 0, 0);
+            const u32x4 y = *reinterpret_cast<const u32x4 *>(x + i * 4);
+            u[i] = there ? make_uint4(y[0], y[1], y[2], y[3]) : make_uint4(0, 0, 0, 0);
         }
     }
     __device__ __forceinline__ void load_singly(const typename Elem<DT>::type *x, int64_t k, int64_t cols, bool there)
@@ -156,7 +157,7 @@ __device__ __forceinline__ void parts_of(const Eight<kF32> &v, bf16x8 (&p)[3])
 // through LDS.  blockIdx.y: the part of the columns (of several, each leaves its sums in `partial`), blockIdx.z: the tokens.
 // Tokens are the matrix instruction's rows, weights its columns, so that a lane needs one row's scales.
 template <int DT, int MT, int BP, int R, int WAVES, int PER_CU>
-__global__ __launch_bounds__(WAVES * 64, WAVES * PER_CU / 4) void product_kernel(const cbinfer_quantised_product_args a, const uint16_t *scales, int blocks, int tiles, int whole, float *partial)
+__global__ __launch_bounds__(WAVES * 64, WAVES * PER_CU / 4) void product_kernel(const cbinfer_quantised_product_args a, const uint16_t *scales, int blocks, int tiles, float *partial)
 {
     typedef typename Elem<DT>::type T;
     constexpr int PARTS = DT == kF32 ? 3 : 1;
@@ -199,13 +200,17 @@ __global__ __launch_bounds__(WAVES * 64, WAVES * PER_CU / 4) void product_kernel
         for (int i = 0; i < BP; ++i) {
             const int64_t k0 = (int64_t)(block0 + i * WAVES) * 128;
             Eight<DT> v[4];
-            if (whole && k0 + 128 <= a.cols) {
+            if (k0 + 128 <= a.cols) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[j].load(row + k0 + j * 32 + (lane >> 4) * 8, t < a.tokens);
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    v[j].load_singly(row, k0 + j * 32 + (lane >> 4) * 8, a.cols, t < a.tokens);
+                    const int64_t k = k0 + j * 32 + (lane >> 4) * 8;
+                    if (k + 8 <= a.cols)
+                        v[j].load(row + k, t < a.tokens);
+                    else
+                        v[j].load_singly(row, k, a.cols, t < a.tokens);
                     asm volatile("" ::: "memory"); // one after the other: together they would take most of the registers
                 }
             }
@@ -311,13 +316,13 @@ struct Shape {
     {
         const int64_t tiles = tiles_of(a.rows), blocks = blocks_of(a.cols), groups = (tiles + R - 1) / R;
         const uint16_t *scales = reinterpret_cast<const uint16_t *>(static_cast<const char *>(a.packed) + code_bytes(a.rows, a.cols));
-        const int whole = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.x_stride * (DT == kF32 ? 4 : 2) % 16 == 0, n = parts(a);
+        const int n = parts(a);
         float *partial = n > 1 ? static_cast<float *>(a.workspace) : nullptr;
         const unsigned z = (unsigned)((a.tokens + 16 * MT - 1) / (16 * MT));
         // as many workgroups as run at a time, each with the same number of turns or one less
         const int64_t room = std::max<int64_t>(1, 256 * PER_CU / (n * z)), turns = (groups + room - 1) / room;
         const dim3 grid((unsigned)((groups + turns - 1) / turns), n, z);
-        product_kernel<DT, MT, BP, R, WAVES, PER_CU><<<grid, WAVES * 64, 0, st>>>(a, scales, (int)blocks, (int)tiles, whole, partial);
+        product_kernel<DT, MT, BP, R, WAVES, PER_CU><<<grid, WAVES * 64, 0, st>>>(a, scales, (int)blocks, (int)tiles, partial);
         if (hipError_t e = hipGetLastError()) return e;
         if (partial) {
             join_parts_kernel<DT><<<dim3((unsigned)((a.rows + 255) / 256), (unsigned)std::min<int64_t>(a.tokens, 1024)), 256, 0, st>>>(a, n, partial);
@@ -327,6 +332,15 @@ struct Shape {
     }
 };
 
+// A wave a block, and as many more workgroups: 54 tokens, 42672 x 168: two waves 12.8 us, eight 19.9; 1 token, 100003 x 512: four 9.0, eight 13.6.
+template <int DT, int MT, int R, typename F>
+auto short_rows(int64_t blocks, F f)
+{
+    if (blocks <= 2) return f(Shape<DT, MT, 1, R, 2, 8>());
+    if (blocks <= 4) return f(Shape<DT, MT, 1, R, 4, 4>());
+    return f(Shape<DT, MT, 1, R, 8, 2>());
+}
+
 // Calls f with the shape for these sizes.  A workgroup's waves times their blocks should be the blocks of a row, or a part of
 // them without much left over: waves without a block wait for the others.
 template <int DT, typename F>
@@ -335,7 +349,7 @@ auto with_shape(const cbinfer_quantised_product_args &a, F f)
     const int64_t tiles = tiles_of(a.rows), blocks = blocks_of(a.cols);
     if constexpr (DT == kBF16) {
         if (a.tokens <= 16) {
-            if (blocks <= 8) return f(Shape<DT, 1, 1, 4, 8, 2>());
+            if (blocks <= 8) return short_rows<DT, 1, 4>(blocks, f);
             if (blocks > 16 && blocks <= 32) {
                 // 1 token, 4096 x 4096: a row's tiles one by one 7.3, in two parts of 8 waves 14; 20000 x 4096: 11.1, two at a time 11.7
                 if (tiles <= 512) return f(Shape<DT, 1, 2, 1, 16, 1>());
@@ -347,7 +361,7 @@ auto with_shape(const cbinfer_quantised_product_args &a, F f)
             return f(Shape<DT, 1, 1, 3, 16, 1>());
         }
         // 17 tokens, 40000 x 1000: 14.1, of 16 waves, half of them without a block, 18.2
-        if (blocks <= 8) return f(Shape<DT, 2, 1, 2, 8, 2>());
+        if (blocks <= 8) return short_rows<DT, 2, 2>(blocks, f);
         // 64 tokens, 100003 x 2048: four tiles of tokens at a time 69, two of 16 waves 83
         if (a.tokens > 32 && tiles >= 1024) return f(Shape<DT, 4, 2, 2, 8, 1>());
         // 64 tokens, 4096 x 4096: 16 waves and a tile at a time, which take rows whole, 10.2, two tiles in two parts 13.7, of 8 waves 14.5
@@ -358,9 +372,9 @@ auto with_shape(const cbinfer_quantised_product_args &a, F f)
         return f(Shape<DT, 2, 1, 2, 16, 1>());
     } else {
         // three parts of x take three times the registers
-        if (a.tokens <= 16 && blocks <= 8) return f(Shape<DT, 1, 1, 4, 8, 2>());
+        if (a.tokens <= 16 && blocks <= 8) return short_rows<DT, 1, 4>(blocks, f);
         // 17 tokens, 40000 x 1000: 16, of 16 waves 25
-        if (blocks <= 8) return f(Shape<DT, 1, 1, 2, 8, 2>());
+        if (blocks <= 8) return short_rows<DT, 1, 2>(blocks, f);
         // 16 tokens, 100003 x 2048: 30.7, of 8 waves 40.6; 36122 x 5669: 44.6, 46.1.  64 tokens, 256 x 38400: 17.7, 8 waves and two tiles of
         // tokens at a time 21.2, four tiles of rows 20.4
         if (a.tokens <= 16 || tiles < 64) return f(Shape<DT, 1, 1, 2, 16, 1>());
