@@ -29,8 +29,8 @@ __device__ __forceinline__ float gate_of(float g, int kind)
     return kind == CBINFER_GATE_SIGMOID ? open : g * open;
 }
 
-// Any size, group, stride and alignment: the row lies in LDS as float32.  One value a thread and load: 8192 rows of 4095 bfloat16
-// with a gate 86 us, where rows of 4096 take 38 in the kernel below.
+// Groups of any size: the row lies in LDS as float32.  One value a thread and load: 8192 rows of 4095 bfloat16 with a gate and groups of
+// 45 158 us, where rows of 4096 in groups of 64 take 42 in the kernel below.
 template <int DT, int DS>
 __global__ __launch_bounds__(256) void norm_row_kernel(const cbinfer_gated_norm_args a, int64_t first)
 {
@@ -74,39 +74,60 @@ __global__ __launch_bounds__(256) void norm_row_kernel(const cbinfer_gated_norm_
     for (int i = threadIdx.x; i < d; i += 256) y[i] = Elem<DT>::put(row[i] * f * a.next_weight[i]);
 }
 
-// Eight values as they lie in memory, 16 bytes at a time.
+// Eight values as they lie in memory, 16 bytes at a time, at any address.
 template <int DT>
 struct Eight {
+    typedef typename Elem<DT>::type T;
+    typedef unsigned Words __attribute__((ext_vector_type(4), aligned(2)));
     uint4 u[DT == kF32 ? 2 : 1];
-    __device__ __forceinline__ void load(const typename Elem<DT>::type *p)
+    __device__ __forceinline__ void load(const T *p)
     {
 #pragma unroll
-        for (int i = 0; i < (DT == kF32 ? 2 : 1); ++i) u[i] = reinterpret_cast<const uint4 *>(p)[i];
+        for (int i = 0; i < (DT == kF32 ? 2 : 1); ++i) {
+            const Words w = *reinterpret_cast<const Words *>(p + 4 * i);
+            u[i] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+    __device__ __forceinline__ void load(const T *p, int n) // of them n, then zeros
+    {
+        union { T e[8]; uint4 u[DT == kF32 ? 2 : 1]; } v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v.e[e] = e < n ? p[e] : T(0);
+#pragma unroll
+        for (int i = 0; i < (DT == kF32 ? 2 : 1); ++i) u[i] = v.u[i];
     }
     __device__ __forceinline__ float get(int e) const { return Unit<DT>::get(u[DT == kF32 ? e / 4 : 0], DT == kF32 ? e % 4 : e); }
-    static __device__ __forceinline__ void store(typename Elem<DT>::type *p, const float (&v)[8])
+    static __device__ __forceinline__ void store(T *p, const float (&v)[8])
     {
         if constexpr (DT == kF32) {
-            reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+#pragma unroll
+            for (int i = 0; i < 8; i += 4)
+                *reinterpret_cast<Words *>(p + i) = Words{__float_as_uint(v[i]), __float_as_uint(v[i + 1]), __float_as_uint(v[i + 2]), __float_as_uint(v[i + 3])};
         } else {
-            *reinterpret_cast<uint4 *>(p) = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+            *reinterpret_cast<Words *>(p) = Words{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
         }
+    }
+    static __device__ __forceinline__ void store(T *p, const float (&v)[8], int n)
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < n) p[e] = Elem<DT>::put(v[e]);
     }
 };
 
-// Rows of whole groups of eight values at 16-byte addresses: TPR threads a row, NV times eight values each, in registers from the
-// first load to the last store.  A workgroup goes on to further rows with the weights it has.
-template <int DT, int DS, int TPR, int NV>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(const cbinfer_gated_norm_args a)
+// Groups of whole eights, or the row as one: TPR threads a row, NV times eight values each, in registers from the
+// first load to the last store.  A workgroup goes on to further rows with the weights it has.  Bound by memory: 8192 rows of 4096
+// with a float32 residual and both norms, 470 MB, 96 us.  TAIL: the last eight of a row is not whole.
+template <int DT, int DS, int TPR, int NV, bool TAIL>
+__global__ __launch_bounds__(TPR < 128 ? 256 : TPR) void norm_kernel(const cbinfer_gated_norm_args a)
 {
     typedef typename Elem<DT>::type T;
     typedef typename Elem<DS>::type R;
-    constexpr int ROWS = TPR < 256 ? 256 / TPR : 1, WAVES = TPR / 64;
+    constexpr int ROWS = TPR < 128 ? 256 / TPR : 1, WAVES = TPR / 64;
     __shared__ float scratch[2][WAVES];
     extern __shared__ float squares[]; // sums of eight squares, where a group is not a power of two lanes
-    const int d = (int)a.size, thread = threadIdx.x % TPR, lane = threadIdx.x & 63, wave = thread >> 6, eights = d / 8;
-    const int share = a.group ? a.group / 8 : eights; // eights of a group
+    const int d = (int)a.size, thread = threadIdx.x % TPR, lane = threadIdx.x & 63, wave = thread >> 6, eights = (d + 7) / 8;
+    const int share = a.group && a.group != d ? a.group / 8 : eights; // eights of a group
     const bool by_lanes = share <= 64 && (share & (share - 1)) == 0, by_row = share == eights;
     int at[NV];
     bool there[NV];
@@ -117,9 +138,10 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(const cbinf
         there[i] = at[i] < d;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            w[i][e] = there[i] && a.weight ? a.weight[at[i] + e] : 1.0f;
-            scale[i][e] = there[i] && a.channel_scale ? a.scale * a.channel_scale[at[i] + e] : a.scale;
-            next[i][e] = there[i] && a.y ? a.next_weight[at[i] + e] : 0.0f;
+            const bool is = TAIL ? at[i] + e < d : there[i];
+            w[i][e] = is && a.weight ? a.weight[at[i] + e] : 1.0f;
+            scale[i][e] = is && a.channel_scale ? a.scale * a.channel_scale[at[i] + e] : a.scale;
+            next[i][e] = is && a.y ? a.next_weight[at[i] + e] : 0.0f;
         }
     }
     auto row_sum = [&](float v, int which) {
@@ -140,7 +162,11 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(const cbinf
         Eight<DS> rs[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            if (there[i]) {
+            if (TAIL && at[i] + 8 > d) {
+                xs[i].load(x + at[i], d - at[i]);
+                if (a.gate) gs[i].load(gate + at[i], d - at[i]);
+                if (a.residual) rs[i].load(residual + at[i], d - at[i]);
+            } else if (there[i]) {
                 xs[i].load(x + at[i]);
                 if (a.gate) gs[i].load(gate + at[i]);
                 if (a.residual) rs[i].load(residual + at[i]);
@@ -182,7 +208,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(const cbinf
                     }
                 if (WAVES > 1) __syncthreads(); else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             }
-            const float each = 8 * share;
+            const float each = by_row ? d : 8 * share;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 f[i] = 1.0f / sqrtf(f[i] / each + a.eps);
@@ -200,7 +226,12 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(const cbinf
                     u[i][e] = a.residual ? __builtin_fmaf(u[i][e], scale[i][e], rs[i].get(e)) : u[i][e] * scale[i][e];
                     sum = __builtin_fmaf(u[i][e], u[i][e], sum);
                 }
-                if (a.h) Eight<DS>::store(static_cast<R *>(a.h) + r * a.h_stride + at[i], u[i]);
+                R *h = static_cast<R *>(a.h) + r * a.h_stride + at[i];
+                if (TAIL && at[i] + 8 > d) {
+                    if (a.h) Eight<DS>::store(h, u[i], d - at[i]);
+                } else if (a.h) {
+                    Eight<DS>::store(h, u[i]);
+                }
             }
         if (a.y) {
             sum = row_sum(sum, 1);
@@ -210,17 +241,21 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(const cbinf
                 if (there[i]) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) u[i][e] *= g * next[i][e];
-                    Eight<DT>::store(static_cast<T *>(a.y) + r * a.y_stride + at[i], u[i]);
+                    T *y = static_cast<T *>(a.y) + r * a.y_stride + at[i];
+                    if (TAIL && at[i] + 8 > d)
+                        Eight<DT>::store(y, u[i], d - at[i]);
+                    else
+                        Eight<DT>::store(y, u[i]);
                 }
         }
         if (WAVES > 1) __syncthreads(); // the sums are read before the next row's come
     }
 }
 
-template <int DT, int DS>
+template <int DT, int DS, bool TAIL>
 hipError_t by_eights(hipStream_t st, const cbinfer_gated_norm_args &a)
 {
-    const int eights = (int)(a.size / 8);
+    const int eights = (int)((a.size + 7) / 8);
     const size_t lds = a.weight && a.group && a.group != a.size ? (size_t)eights * sizeof(float) : 0;
     // A workgroup reads the weights once for all its rows: few of them pay, if they still cover the memory's latency.  us for 8192
     // rows of 4096 with a float32 residual and both norms (470 MB) at 256, 512, 768, 1024, 8192 workgroups: 124, 96, 106, 111, 214;
@@ -228,25 +263,24 @@ hipError_t by_eights(hipStream_t st, const cbinfer_gated_norm_args &a)
     const int waves = a.y ? 2048 : 4096;
     auto blocks = [&](int threads, int rows) { return (unsigned)std::min<int64_t>((a.rows + rows - 1) / rows, std::max(256, waves * 64 / threads)); };
     if (eights <= 64)
-        norm_kernel<DT, DS, 64, 1><<<blocks(256, 4), 256, 4 * lds, st>>>(a);
+        norm_kernel<DT, DS, 64, 1, TAIL><<<blocks(256, 4), 256, 4 * lds, st>>>(a);
+    else if (eights <= 128) // 4000 rows of 527 bfloat16, a residual and both norms: 21 us, 256 threads a row 32
+        norm_kernel<DT, DS, 128, 1, TAIL><<<blocks(128, 1), 128, lds, st>>>(a);
     else if (eights <= 256)
-        norm_kernel<DT, DS, 256, 1><<<blocks(256, 1), 256, lds, st>>>(a);
+        norm_kernel<DT, DS, 256, 1, TAIL><<<blocks(256, 1), 256, lds, st>>>(a);
     else if (eights <= 512)
-        norm_kernel<DT, DS, 256, 2><<<blocks(256, 1), 256, lds, st>>>(a);
+        norm_kernel<DT, DS, 256, 2, TAIL><<<blocks(256, 1), 256, lds, st>>>(a);
     else if (eights <= 1024)
-        norm_kernel<DT, DS, 512, 2><<<blocks(512, 1), 512, lds, st>>>(a);
+        norm_kernel<DT, DS, 512, 2, TAIL><<<blocks(512, 1), 512, lds, st>>>(a);
     else
-        norm_kernel<DT, DS, 1024, 2><<<blocks(1024, 1), 1024, lds, st>>>(a);
+        norm_kernel<DT, DS, 1024, 2, TAIL><<<blocks(1024, 1), 1024, lds, st>>>(a);
     return hipGetLastError();
 }
 
-// Whether every row that is there begins at a 16-byte address.
-bool in_eights(const cbinfer_gated_norm_args &a)
+template <bool TAIL>
+hipError_t by_eights(hipStream_t st, const cbinfer_gated_norm_args &a)
 {
-    const size_t e = a.dtype == kF32 ? 4 : 2, s = a.sum_dtype == kF32 ? 4 : 2;
-    auto fits = [](const void *p, int64_t stride, size_t size) { return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * (int64_t)size % 16 == 0); };
-    return a.size % 8 == 0 && a.group % 8 == 0 && fits(a.x, a.x_stride, e) && fits(a.gate, a.gate_stride, e) && fits(a.y, a.y_stride, e) &&
-           fits(a.residual, a.residual_stride, s) && fits(a.h, a.h_stride, s);
+    return a.dtype == kF32 ? by_eights<kF32, kF32, TAIL>(st, a) : a.sum_dtype == kF32 ? by_eights<kBF16, kF32, TAIL>(st, a) : by_eights<kBF16, kBF16, TAIL>(st, a);
 }
 
 constexpr int64_t kMostBlocks = 1 << 22; // of a launch: threads are counted in 32 bits
@@ -255,8 +289,7 @@ constexpr int64_t kMostBlocks = 1 << 22; // of a launch: threads are counted in 
 
 hipError_t gated_norm(hipStream_t st, const cbinfer_gated_norm_args &a)
 {
-    if (in_eights(a))
-        return a.dtype == kF32 ? by_eights<kF32, kF32>(st, a) : a.sum_dtype == kF32 ? by_eights<kBF16, kF32>(st, a) : by_eights<kBF16, kBF16>(st, a);
+    if (a.group == 0 || a.group == a.size || a.group % 8 == 0) return a.size % 8 == 0 ? by_eights<false>(st, a) : by_eights<true>(st, a);
     const int groups = a.group ? (int)(a.size / a.group) : 1;
     const size_t lds = (size_t)(a.size + groups + 4) * sizeof(float);
     auto kernel = a.dtype == kF32 ? norm_row_kernel<kF32, kF32> : a.sum_dtype == kF32 ? norm_row_kernel<kBF16, kF32> : norm_row_kernel<kBF16, kBF16>;

@@ -123,3 +123,11 @@ def test_nothing_to_do_and_other_streams():
         got = cb.gated_norm(t["x"], t["weight"], group=128, residual=t["residual"], next_weight=t["next"])
     side.synchronize()
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("kind,sum_kind", KINDS)
+@pytest.mark.parametrize("rows,d", [(9, 5), (3000, 513), (5, 519), (2100, 1023), (3, 1025), (2, 2049), (3, 4095), (2, 4097), (2, 8191), (1, 16383)])
+def test_rows_that_end_inside_eight(rows, d, kind, sum_kind):
+    t = _all(rows, d, kind, sum_kind)
+    kw = dict(weight=t["weight"], gate=t["gate"], activation="sigmoid", residual=t["residual"], scale=t["channel"], next_weight=t["next"])
+    _check(*cb.gated_norm(t["x"], **kw), t["x"], "%dx%d" % (rows, d), **kw)
