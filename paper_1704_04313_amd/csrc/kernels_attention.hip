@@ -599,13 +599,18 @@ Plan plan(const cbinfer_linear_attention_args &a)
     if (a.tokens < 16 || (a.dtype == kF32 && a.key_size > 128)) return p; // float32 rows of 256 keys do not fit LDS
     p.chunks = true;
     const int tiles = (a.value_size + 31) / 32;
-    p.tiles = tiles <= 2 && a.key_size <= 128 ? 2 : 4;
+    const int64_t heads = (int64_t)a.streams * a.heads, chunks = (a.tokens + kChunk - 1) / kChunk;
+    // Two tiles where all chunks together do not fill the chip twice: their scores are computed twice, but four waves are through sooner
+    // than eight.  us for 82 tokens, 4 heads of 96 x 128 float32: 24, four tiles 28; 8192 tokens, 16 heads: 99, 72.
+    p.tiles = a.key_size <= 128 && (tiles <= 2 || heads * ((tiles + 1) / 2) * chunks <= 512) ? 2 : 4;
     p.slices = (tiles + p.tiles - 1) / p.tiles;
-    const int64_t groups = (int64_t)a.streams * a.heads * p.slices, chunks = (a.tokens + kChunk - 1) / kChunk;
+    const int64_t groups = heads * p.slices;
     // Parts until every compute unit has a workgroup; their keys and values are read twice.  us for 8192 tokens, 16 heads of 128: 8 parts 119,
-    // 16 78, 32 93.  Streams of different lengths leave compute units idle: two and a half times as many (12 streams of up to 1023 tokens,
-    // 6 heads, float32: 3 parts 83, 6 69, 8 62, 16 66).
-    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(chunks / 2, (a.lengths ? 640 : 256) / std::max<int64_t>(groups, 1)));
+    // 16 72, 20 96.  Streams of different lengths leave compute units idle: half as many again (12 streams of up to 1023 tokens, 6 heads,
+    // float32: 3 parts 83, 6 62, 7 70, 8 64; 8 of up to 600, 16 heads of 128, bfloat16: 3 parts 47, 5 55).  Two launches more pay from four
+    // chunks on, float32 from three (2 streams of 190 tokens, 16 heads of 128, bfloat16: 15.5, in parts 23; one of 147, 2 heads, float32: 34, 24).
+    const int64_t most = chunks > (a.dtype == kF32 ? 2 : 3) ? chunks : 1;
+    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(most, (a.lengths ? 400 : 256) / std::max<int64_t>(groups, 1)));
     p.per = (int)((chunks + p.parts - 1) / p.parts);
     p.parts = (int)((chunks + p.per - 1) / p.per);
     return p;
