@@ -65,7 +65,8 @@ int cbinfer_log_probs(const cbinfer_log_probs_args *a, void *stream);
  * left in its place.  Head h reads the keys and values of head h / (heads / kv_heads).  q [streams][tokens][heads][key_size],
  * k [streams][tokens][kv_heads][key_size], v [streams][tokens][kv_heads][value_size], o like q with value_size:
  * strides of the first three axes are given, the last axis is contiguous.  A stream of length 0 keeps its state; o is 0
- * from a stream's length on, where q, k and v are not read. */
+ * from a stream's length on, where q, k and v are not read.  A value that is not finite makes its column of S infinite or NaN,
+ * a key its row, and the outputs that follow; earlier outputs stay as they are. */
 typedef struct {
     int32_t dtype;                                      /* of q, k, v, o */
     int32_t streams, tokens, heads, kv_heads;           /* each >= 0; heads a multiple of kv_heads */
@@ -105,7 +106,7 @@ int cbinfer_pack_weights(const uint8_t *codes, const uint16_t *scales, int64_t r
 typedef struct {
     int32_t dtype;                                      /* of x and y */
     int32_t group;
-    int64_t tokens, rows, cols;                         /* x [tokens][cols], y [tokens][rows]; rows, cols >= 1 */
+    int64_t tokens, rows, cols;                         /* x [tokens][cols], y [tokens][rows]; 0 .. 2^19, 1 .. 2^26, 1 .. 2^25 */
     int64_t x_stride, y_stride;                         /* from token to token */
     const void *x;
     const void *packed;
