@@ -115,18 +115,19 @@ struct Eight {
     }
 };
 
-// Groups of whole eights, or the row as one: TPR threads a row, NV times eight values each, in registers from the
-// first load to the last store.  A workgroup goes on to further rows with the weights it has.  Bound by memory: 8192 rows of 4096
+// Groups of whole eights, or the row as one: a wave a row (MOST 64, four rows a workgroup) or a workgroup of up to MOST threads, as
+// many waves as the row needs; NV times eight values a thread, in registers from the first load to the last store.  A workgroup goes on to further rows with the weights it has.  Bound by memory: 8192 rows of 4096
 // with a float32 residual and both norms, 470 MB, 96 us.  TAIL: the last eight of a row is not whole.
-template <int DT, int DS, int TPR, int NV, bool TAIL>
-__global__ __launch_bounds__(TPR < 128 ? 256 : TPR) void norm_kernel(const cbinfer_gated_norm_args a)
+template <int DT, int DS, int MOST, int NV, bool TAIL>
+__global__ __launch_bounds__(MOST < 256 ? 256 : MOST) void norm_kernel(const cbinfer_gated_norm_args a)
 {
     typedef typename Elem<DT>::type T;
     typedef typename Elem<DS>::type R;
-    constexpr int ROWS = TPR < 128 ? 256 / TPR : 1, WAVES = TPR / 64;
+    constexpr int ROWS = MOST < 256 ? 256 / MOST : 1, WAVES = MOST / 64;
     __shared__ float scratch[2][WAVES];
+    const int threads = ROWS > 1 ? MOST : blockDim.x; // of a row
     extern __shared__ float squares[]; // sums of eight squares, where a group is not a power of two lanes
-    const int d = (int)a.size, thread = threadIdx.x % TPR, lane = threadIdx.x & 63, wave = thread >> 6, eights = (d + 7) / 8;
+    const int d = (int)a.size, thread = ROWS > 1 ? threadIdx.x % MOST : threadIdx.x, lane = threadIdx.x & 63, wave = thread >> 6, eights = (d + 7) / 8;
     const int share = a.group && a.group != d ? a.group / 8 : eights; // eights of a group
     const bool by_lanes = share <= 64 && (share & (share - 1)) == 0, by_row = share == eights;
     int at[NV];
@@ -134,7 +135,7 @@ __global__ __launch_bounds__(TPR < 128 ? 256 : TPR) void norm_kernel(const cbinf
     float w[NV][8], scale[NV][8], next[NV][8];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        at[i] = (i * TPR + thread) * 8;
+        at[i] = (i * threads + thread) * 8;
         there[i] = at[i] < d;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -151,11 +152,11 @@ __global__ __launch_bounds__(TPR < 128 ? 256 : TPR) void norm_kernel(const cbinf
             __syncthreads();
             v = 0.0f;
 #pragma unroll
-            for (int i = 0; i < WAVES; ++i) v += scratch[which][i];
+            for (int i = 0; i < WAVES; ++i) v += i * 64 < threads ? scratch[which][i] : 0.0f;
         }
         return v;
     };
-    for (int64_t r = (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? threadIdx.x / TPR : 0); r < a.rows; r += (int64_t)gridDim.x * ROWS) {
+    for (int64_t r = (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? threadIdx.x / MOST : 0); r < a.rows; r += (int64_t)gridDim.x * ROWS) {
         const T *x = static_cast<const T *>(a.x) + r * a.x_stride, *gate = static_cast<const T *>(a.gate) + r * a.gate_stride;
         const R *residual = static_cast<const R *>(a.residual) + r * a.residual_stride;
         Eight<DT> xs[NV], gs[NV];
@@ -194,7 +195,7 @@ __global__ __launch_bounds__(TPR < 128 ? 256 : TPR) void norm_kernel(const cbinf
                 for (int i = 0; i < NV; ++i)
                     for (int off = share / 2; off; off >>= 1) f[i] += __shfl_xor(f[i], off);
             } else {
-                float *mine = squares + (ROWS > 1 ? threadIdx.x / TPR : 0) * eights;
+                float *mine = squares + (ROWS > 1 ? threadIdx.x / MOST : 0) * eights;
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
                     if (there[i]) mine[at[i] / 8] = f[i];
@@ -261,19 +262,20 @@ hipError_t by_eights(hipStream_t st, const cbinfer_gated_norm_args &a)
     // rows of 4096 with a float32 residual and both norms (470 MB) at 256, 512, 768, 1024, 8192 workgroups: 124, 96, 106, 111, 214;
     // 8192 of 2048 with groups of 128 and a gate alone (101 MB): 42, 26, 23, 22, 34.
     const int waves = a.y ? 2048 : 4096;
-    auto blocks = [&](int threads, int rows) { return (unsigned)std::min<int64_t>((a.rows + rows - 1) / rows, std::max(256, waves * 64 / threads)); };
+    // 8192 rows of 768 bfloat16, a residual and both norms: two waves a row 23 us, four 34
+    const int threads = eights <= 64 ? 256 : ((eights <= 256 ? eights : (eights + 1) / 2) + 63) / 64 * 64, rows = eights <= 64 ? 4 : 1;
+    const int each = std::max(1, (waves * 64 + 128 * threads) / (256 * threads)); // of a compute unit, all the same
+    const unsigned blocks = (unsigned)std::min<int64_t>((a.rows + rows - 1) / rows, 256 * each);
     if (eights <= 64)
-        norm_kernel<DT, DS, 64, 1, TAIL><<<blocks(256, 4), 256, 4 * lds, st>>>(a);
-    else if (eights <= 128) // 4000 rows of 527 bfloat16, a residual and both norms: 21 us, 256 threads a row 32
-        norm_kernel<DT, DS, 128, 1, TAIL><<<blocks(128, 1), 128, lds, st>>>(a);
+        norm_kernel<DT, DS, 64, 1, TAIL><<<blocks, threads, 4 * lds, st>>>(a);
     else if (eights <= 256)
-        norm_kernel<DT, DS, 256, 1, TAIL><<<blocks(256, 1), 256, lds, st>>>(a);
+        norm_kernel<DT, DS, 256, 1, TAIL><<<blocks, threads, lds, st>>>(a);
     else if (eights <= 512)
-        norm_kernel<DT, DS, 256, 2, TAIL><<<blocks(256, 1), 256, lds, st>>>(a);
+        norm_kernel<DT, DS, 256, 2, TAIL><<<blocks, threads, lds, st>>>(a);
     else if (eights <= 1024)
-        norm_kernel<DT, DS, 512, 2, TAIL><<<blocks(512, 1), 512, lds, st>>>(a);
+        norm_kernel<DT, DS, 512, 2, TAIL><<<blocks, threads, lds, st>>>(a);
     else
-        norm_kernel<DT, DS, 1024, 2, TAIL><<<blocks(1024, 1), 1024, lds, st>>>(a);
+        norm_kernel<DT, DS, 1024, 2, TAIL><<<blocks, threads, lds, st>>>(a);
     return hipGetLastError();
 }
 
