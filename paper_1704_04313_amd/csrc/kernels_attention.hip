@@ -224,11 +224,18 @@ __device__ __forceinline__ int swizzle(int row)
     return KT == 2 ? (row & 2) << 1 | (row >> 2 & 3) : (row & 3) << 2 | (row >> 2 & 3);
 }
 
+// Outputs and states are sums over the keys' values: float32 keys of more than 128, of which a chunk does not fit LDS, are taken in
+// pieces, each with its rows of the states, and every piece after the first adds to the outputs.
+struct Keys {
+    int64_t state; // from a head's state to the next
+    bool add;
+};
+
 // OUT: outputs of the tokens of a part (`per` chunks) of the sequence, from the state in front of it.  Otherwise what those
 // tokens leave in a state of zero, where further tokens follow.  `states`: [stream][head][part][key_size][value_size].
 // WHOLE: rows are pieces of 16 bytes at 16-byte addresses.
 template <int DT, int KT, int NC, bool OUT, bool WHOLE>
-__global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_attention_args a, int slices, int per, int parts, float *states)
+__global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_attention_args a, int slices, int per, int parts, float *states, Keys keys)
 {
     typedef typename Elem<DT>::type T;
     typedef ChunkLds<DT, KT, NC, OUT> Lds;
@@ -315,7 +322,7 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
     const unsigned state_bytes = (unsigned)(dk * dv) * 4, state_at = column < dv ? (unsigned)(row0 * dv + column) * 4 : kBeyond;
     auto place = [&](int kt, int r) { return state_at + (unsigned)((32 * kt + 8 * (r / 4) + r % 4) * dv) * 4; };
     f32x16 S[KH] = {};
-    float *state = a.state + (int64_t)bh * dk * dv;
+    float *state = a.state + bh * keys.state;
     if (OUT) {
         const Buffer from = buffer(parts > 1 ? states + ((int64_t)bh * parts + part) * dk * dv : state, state_bytes);
 #pragma unroll
@@ -542,6 +549,7 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const unsigned at = from + (8 * (r / 4) + r % 4) * each;
+                    if (DT == kF32 && keys.add) acc[r] += __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(to, at, 0, 0));
                     if constexpr (DT == kBF16)
                         __builtin_amdgcn_raw_buffer_store_b16(Elem<DT>::put(acc[r]), to, at, 0, 0);
                     else
@@ -551,7 +559,10 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
                 T *to = o + (int64_t)(t + i0) * a.o_stride[1] + column;
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (i0 + 8 * (r / 4) + r % 4 < m && column < dv) to[(8 * (r / 4) + r % 4) * a.o_stride[1]] = Elem<DT>::put(acc[r]);
+                    if (i0 + 8 * (r / 4) + r % 4 < m && column < dv) {
+                        T &x = to[(8 * (r / 4) + r % 4) * a.o_stride[1]];
+                        x = Elem<DT>::put(DT == kF32 && keys.add ? acc[r] + Elem<DT>::get(x) : acc[r]);
+                    }
             }
         }
     }
@@ -567,13 +578,13 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
 
 // What the parts of a sequence leave by themselves (places 1, 2, ...) becomes the states in front of the parts.  Bound by memory:
 // 16 heads of 128 x 128 in 16 parts, 33 MB, 8 us.
-__global__ __launch_bounds__(256) void join_parts_kernel(const cbinfer_linear_attention_args a, int per, int parts, float *states)
+__global__ __launch_bounds__(256) void join_parts_kernel(const cbinfer_linear_attention_args a, int per, int parts, float *states, Keys keys)
 {
     const int bh = blockIdx.y, size = a.key_size * a.value_size, at = blockIdx.x * 256 + threadIdx.x, b = bh / a.heads;
     if (at >= size) return;
     const int n = a.lengths ? min(max(a.lengths[b], 0), a.tokens) : a.tokens;
     const float g = power(a.decay[bh - b * a.heads], per * kChunk);
-    float *s = states + (int64_t)bh * parts * size + at, x = a.state[(int64_t)bh * size + at];
+    float *s = states + (int64_t)bh * parts * size + at, x = a.state[bh * keys.state + at];
     const int last = (int)min((int64_t)parts, ((int64_t)n + per * kChunk - 1) / (per * kChunk)); // parts with tokens
     s[0] = x;
     for (int p0 = 1; p0 < last; p0 += 8) { // eight loads on their way at a time
@@ -596,13 +607,13 @@ struct Plan {
 Plan plan(const cbinfer_linear_attention_args &a)
 {
     Plan p = {false, 1, 1, 1, 4};
-    if (a.tokens < 16 || (a.dtype == kF32 && a.key_size > 128)) return p; // float32 rows of 256 keys do not fit LDS
+    if (a.tokens < 16) return p;
     p.chunks = true;
     const int tiles = (a.value_size + 31) / 32;
     const int64_t heads = (int64_t)a.streams * a.heads, chunks = (a.tokens + kChunk - 1) / kChunk;
     // Two tiles where all chunks together do not fill the chip twice: their scores are computed twice, but four waves are through sooner
     // than eight.  us for 82 tokens, 4 heads of 96 x 128 float32: 24, four tiles 28; 8192 tokens, 16 heads: 99, 72.
-    p.tiles = a.key_size <= 128 && (tiles <= 2 || heads * ((tiles + 1) / 2) * chunks <= 512) ? 2 : 4;
+    p.tiles = (a.dtype == kF32 || a.key_size <= 128) && (tiles <= 2 || heads * ((tiles + 1) / 2) * chunks <= 512) ? 2 : 4;
     p.slices = (tiles + p.tiles - 1) / p.tiles;
     const int64_t groups = heads * p.slices;
     // Parts until every compute unit has a workgroup; their keys and values are read twice.  us for 8192 tokens, 16 heads of 128: 8 parts 119,
@@ -617,27 +628,39 @@ Plan plan(const cbinfer_linear_attention_args &a)
 }
 
 template <int DT, int KT, int NC, bool WHOLE>
-hipError_t chunked(hipStream_t st, const cbinfer_linear_attention_args &a, const Plan &p)
+hipError_t chunked(hipStream_t st, const cbinfer_linear_attention_args &a, const Plan &p, const Keys &keys)
 {
     float *states = static_cast<float *>(a.workspace);
     const unsigned groups = (unsigned)(a.streams * a.heads * p.slices);
     if (p.parts > 1) {
-        chunk_kernel<DT, KT, NC, false, WHOLE><<<dim3(groups, p.parts - 1), NC * 128, 0, st>>>(a, p.slices, p.per, p.parts, states);
+        chunk_kernel<DT, KT, NC, false, WHOLE><<<dim3(groups, p.parts - 1), NC * 128, 0, st>>>(a, p.slices, p.per, p.parts, states, keys);
         if (hipError_t err = hipGetLastError()) return err;
-        join_parts_kernel<<<dim3((a.key_size * a.value_size + 255) / 256, a.streams * a.heads), 256, 0, st>>>(a, p.per, p.parts, states);
+        join_parts_kernel<<<dim3((a.key_size * a.value_size + 255) / 256, a.streams * a.heads), 256, 0, st>>>(a, p.per, p.parts, states, keys);
         if (hipError_t err = hipGetLastError()) return err;
     }
-    chunk_kernel<DT, KT, NC, true, WHOLE><<<dim3(groups, p.parts), NC * 128, 0, st>>>(a, p.slices, p.per, p.parts, states);
+    chunk_kernel<DT, KT, NC, true, WHOLE><<<dim3(groups, p.parts), NC * 128, 0, st>>>(a, p.slices, p.per, p.parts, states, keys);
     return hipGetLastError();
 }
+
+constexpr int kKeys = 128; // at a time, float32
 
 template <int DT, bool WHOLE>
 hipError_t chunked_any(hipStream_t st, const cbinfer_linear_attention_args &a, const Plan &p)
 {
-    if (a.key_size <= 64) return p.tiles == 2 ? chunked<DT, 2, 2, WHOLE>(st, a, p) : chunked<DT, 2, 4, WHOLE>(st, a, p);
-    if (a.key_size <= 128) return p.tiles == 2 ? chunked<DT, 4, 2, WHOLE>(st, a, p) : chunked<DT, 4, 4, WHOLE>(st, a, p);
-    if constexpr (DT == kBF16) return chunked<DT, 8, 4, WHOLE>(st, a, p);
-    return hipErrorInvalidValue;
+    if constexpr (DT == kBF16)
+        if (a.key_size > 128) return chunked<DT, 8, 4, WHOLE>(st, a, p, {(int64_t)a.key_size * a.value_size, false});
+    for (int k0 = 0; k0 < a.key_size; k0 += kKeys) { // once but for float32 keys of more than 128
+        cbinfer_linear_attention_args b = a;
+        b.key_size = std::min(a.key_size - k0, kKeys);
+        b.q = static_cast<const typename Elem<DT>::type *>(a.q) + k0;
+        b.k = static_cast<const typename Elem<DT>::type *>(a.k) + k0;
+        b.state = a.state + (int64_t)k0 * a.value_size;
+        const Keys keys = {(int64_t)a.key_size * a.value_size, k0 > 0};
+        const hipError_t err = b.key_size <= 64 ? p.tiles == 2 ? chunked<DT, 2, 2, WHOLE>(st, b, p, keys) : chunked<DT, 2, 4, WHOLE>(st, b, p, keys)
+                                                : p.tiles == 2 ? chunked<DT, 4, 2, WHOLE>(st, b, p, keys) : chunked<DT, 4, 4, WHOLE>(st, b, p, keys);
+        if (err) return err;
+    }
+    return hipSuccess;
 }
 
 template <int DT>
@@ -660,7 +683,8 @@ hipError_t chunked_any(hipStream_t st, const cbinfer_linear_attention_args &a, c
 size_t linear_attention_workspace(const cbinfer_linear_attention_args &a)
 {
     const Plan p = plan(a);
-    return p.parts > 1 ? (size_t)a.streams * a.heads * p.parts * a.key_size * a.value_size * sizeof(float) : 0;
+    const int keys = a.dtype == kF32 ? std::min(a.key_size, kKeys) : a.key_size;
+    return p.parts > 1 ? (size_t)a.streams * a.heads * p.parts * keys * a.value_size * sizeof(float) : 0;
 }
 
 hipError_t linear_attention(hipStream_t st, const cbinfer_linear_attention_args &a)

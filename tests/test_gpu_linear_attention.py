@@ -143,3 +143,10 @@ def test_output_given_and_no_tokens():
     assert out.data_ptr() == wide.data_ptr() and bool((wide[..., 32:] == 7.0).all())
     att.reset()
     torch.testing.assert_close(att.process(q, q, q), cb.LinearAttention([0.9] * 2, 32, 32, n_streams=2).process(q, q, q), rtol=0, atol=0)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dk,dv", [(129, 33), (192, 64), (256, 128), (200, 130)])
+def test_prompts_with_long_keys(dk, dv, dtype):
+    _run(1, 400, 3, 1, dk, dv, dtype, what="long keys")
+    _run(4, 300, 2, 2, dk, dv, dtype, lengths=[300, 0, 64, 131], what="long keys, ragged")
