@@ -201,11 +201,10 @@ __device__ __forceinline__ float power(float g, int n)
 template <int DT, int KT, int NC, bool OUT>
 struct alignas(16) ChunkLds {
     typedef typename Elem<DT>::type T;
-    // Rows are longer so that the lanes of an access reach different banks: 16 bytes where each lane reads 16 of a row of its own,
-    // 64 where four rows are read across (bfloat16 K and V, transposed on the way).
-    static constexpr int K = 32 * KT, V = 32 * NC, PAD = 16 / (int)sizeof(T), ACROSS = DT == kBF16 ? 32 : PAD;
-    static constexpr int KPAD = DT == kBF16 ? 0 : PAD; // bfloat16: see swizzle()
-    T k[kChunk][K + KPAD], v[kChunk][V + ACROSS], q[OUT ? kChunk : 1][K + PAD];
+    // Rows are 16 bytes longer so that lanes which read as much of a row each reach different banks; bfloat16 K and V are read across
+    // their rows too, see swizzle().
+    static constexpr int K = 32 * KT, V = 32 * NC, PAD = 16 / (int)sizeof(T), ACROSS = DT == kBF16 ? 0 : PAD;
+    T k[kChunk][K + ACROSS], v[kChunk][V + ACROSS], q[OUT ? kChunk : 1][K + PAD];
     T p[DT == kBF16 ? 2 : 1][OUT ? kChunk : 1][kChunk + PAD]; // scores, by query; bfloat16: in two parts
     f32x4 other[OUT ? 2 * NC : 1][4][64]; // a wave's part of Q S for the queries of the wave beside it
     float fade_v[kChunk];        // g^(m-1) ... g^0 of the chunk at hand, then ones
@@ -224,6 +223,13 @@ __device__ __forceinline__ int swizzle(int row)
     return KT == 2 ? (row & 2) << 1 | (row >> 2 & 3) : (row & 3) << 2 | (row >> 2 & 3);
 }
 
+// V is read across its rows alone: what to exclusive-or a column with.
+template <int NC>
+__device__ __forceinline__ int swizzle_across(int row)
+{
+    return NC == 2 ? (row & 2) << 4 : (row & 3) << 5;
+}
+
 // Outputs and states are sums over the keys' values: float32 keys of more than 128, of which a chunk does not fit LDS, are taken in
 // pieces, each with its rows of the states, and every piece after the first adds to the outputs.
 struct Keys {
@@ -235,7 +241,7 @@ struct Keys {
 // tokens leave in a state of zero, where further tokens follow.  `states`: [stream][head][part][key_size][value_size].
 // WHOLE: rows are pieces of 16 bytes at 16-byte addresses.
 template <int DT, int KT, int NC, bool OUT, bool WHOLE>
-__global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_attention_args a, int slices, int per, int parts, float *states, Keys keys)
+__global__ __launch_bounds__(NC * 128, NC == 4 || DT == kBF16 ? 2 : 1) void chunk_kernel(const cbinfer_linear_attention_args a, int slices, int per, int parts, float *states, Keys keys)
 {
     typedef typename Elem<DT>::type T;
     typedef ChunkLds<DT, KT, NC, OUT> Lds;
@@ -351,7 +357,7 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
             }
         }
 #pragma unroll
-        for (int i = 0; i < VP; ++i) *reinterpret_cast<u32x4 *>(&lds.v[vrow + i * VR][vcol]) = vr[i];
+        for (int i = 0; i < VP; ++i) *reinterpret_cast<u32x4 *>(&lds.v[vrow + i * VR][DT == kBF16 ? vcol ^ swizzle_across<NC>(vrow + i * VR) : vcol]) = vr[i];
         if (OUT) {
             bool odd = false;
             if (DT == kBF16) {
@@ -381,8 +387,9 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
         if constexpr (DT == kBF16) {
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
-                const T *from = &lds.v[16 * s + 8 * half + (lane & 15) / 4][tile * 32 + (lane & 16) + 4 * (lane & 3)];
-                const uint2 x = across_rows(from), y = across_rows(from + 4 * (Lds::V + Lds::ACROSS));
+                const int row = 8 * half + (lane & 15) / 4;
+                const T *from = &lds.v[16 * s + row][(tile * 32 + (lane & 16) + 4 * (lane & 3)) ^ swizzle_across<NC>(row)];
+                const uint2 x = across_rows(from), y = across_rows(from + 4 * Lds::V);
                 vs[s] = u32x4{x.x, x.y, y.x, y.y};
             }
         } else {
@@ -531,7 +538,7 @@ __global__ __launch_bounds__(NC * 128) void chunk_kernel(const cbinfer_linear_at
                 }
             } else { // a value that is not finite: its product with the score 0 of an earlier token must not be added
                 for (int j = 0; j < m; ++j) {
-                    const float x = Elem<DT>::get(lds.v[j][tile * 32 + side]);
+                    const float x = Elem<DT>::get(lds.v[j][DT == kBF16 ? (tile * 32 + side) ^ swizzle_across<NC>(j) : tile * 32 + side]);
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int i = i0 + 8 * (r / 4) + r % 4;
@@ -621,7 +628,9 @@ Plan plan(const cbinfer_linear_attention_args &a)
     // float32: 3 parts 83, 6 62, 7 70, 8 64; 8 of up to 600, 16 heads of 128, bfloat16: 3 parts 47, 5 55).  Two launches more pay from four
     // chunks on, float32 from three (2 streams of 190 tokens, 16 heads of 128, bfloat16: 15.5, in parts 23; one of 147, 2 heads, float32: 34, 24).
     const int64_t most = chunks > (a.dtype == kF32 ? 2 : 3) ? chunks : 1;
-    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(most, (a.lengths ? 400 : 256) / std::max<int64_t>(groups, 1)));
+    // Of two tiles in bfloat16 a compute unit takes two workgroups (6 streams of 1749 tokens, 12 heads of 96 x 64: 52, with one 67).
+    const int64_t room = (a.lengths ? 400 : 256) * (p.tiles == 2 && a.dtype == kBF16 ? 2 : 1);
+    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(most, room / std::max<int64_t>(groups, 1)));
     p.per = (int)((chunks + p.parts - 1) / p.parts);
     p.parts = (int)((chunks + p.per - 1) / p.per);
     return p;
