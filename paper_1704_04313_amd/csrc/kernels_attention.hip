@@ -625,12 +625,17 @@ Plan plan(const cbinfer_linear_attention_args &a)
     const int64_t groups = heads * p.slices;
     // Parts until every compute unit has a workgroup; their keys and values are read twice.  us for 8192 tokens, 16 heads of 128: 8 parts 119,
     // 16 72, 20 96.  Streams of different lengths leave compute units idle: half as many again (12 streams of up to 1023 tokens, 6 heads,
-    // float32: 3 parts 83, 6 62, 7 70, 8 64; 8 of up to 600, 16 heads of 128, bfloat16: 3 parts 47, 5 55).  Two launches more pay from four
-    // chunks on, float32 from three (2 streams of 190 tokens, 16 heads of 128, bfloat16: 15.5, in parts 23; one of 147, 2 heads, float32: 34, 24).
-    const int64_t most = chunks > (a.dtype == kF32 ? 2 : 3) ? chunks : 1;
-    // Of two tiles in bfloat16 a compute unit takes two workgroups (6 streams of 1749 tokens, 12 heads of 96 x 64: 52, with one 67).
+    // float32: 3 parts 83, 6 62, 7 70, 8 64).  Of two tiles in bfloat16 a compute unit takes two workgroups (6 streams of 1749 tokens, 12 heads
+    // of 96 x 64: 52, with one 67).
     const int64_t room = (a.lengths ? 400 : 256) * (p.tiles == 2 && a.dtype == kBF16 ? 2 : 1);
-    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(most, room / std::max<int64_t>(groups, 1)));
+    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(chunks, room / std::max<int64_t>(groups, 1)));
+    // Whether they pay, in us as measured: a chunk takes `each`, and 0.7 of it again in a part; two more launches 8, a state 8 bytes a value
+    // at 4.5 TB/s.  8 streams of 600 tokens, 16 heads of 128 x 128: 45, in two parts 62; 16 of 500 tokens, 16 of 64 x 64: 28, 39; 4 of 1000
+    // tokens, 16 of 128 x 128: 63, in four 48; one of 147 tokens, 2 heads, float32: 34, in three 24.
+    const float each = a.dtype == kF32 ? (a.key_size > 64 ? 11.0f : 7.5f) : a.key_size > 128 ? 8.0f : p.tiles == 4 ? 4.3f : a.key_size > 64 ? 3.6f : 2.9f;
+    const float side = groups * p.parts > 256 && room > 400 ? 0.7f * p.parts : p.parts; // by side: the second workgroup of a unit is worth less
+    const float gain = chunks * each * (1.0f - 1.7f / side) * (a.lengths ? 0.75f : 1.0f);
+    if (gain < 8.0f + heads * p.parts * (float)a.key_size * a.value_size * 8.0f / 4.5e6f) p.parts = 1;
     p.per = (int)((chunks + p.parts - 1) / p.parts);
     p.parts = (int)((chunks + p.per - 1) / p.per);
     return p;
