@@ -362,8 +362,14 @@ auto with_shape(const cbinfer_quantised_product_args &a, F f)
         }
         // 17 tokens, 40000 x 1000: 14.1, of 16 waves, half of them without a block, 18.2
         if (blocks <= 8) return short_rows<DT, 2, 2>(blocks, f);
-        // 64 tokens, 100003 x 2048: four tiles of tokens at a time 69, two of 16 waves 83
-        if (a.tokens > 32 && tiles >= 1024) return f(Shape<DT, 4, 2, 2, 8, 1>());
+        if (a.tokens > 32 && tiles >= 1024) {
+            // three tiles of tokens at a time, 48 tokens, 100003 x 2048: 47, four 58; 37 tokens, 56488 x 1310: 29, 35
+            if (a.tokens <= 48) return f(Shape<DT, 3, 2, 2, 8, 1>());
+            // 64 tokens, 100003 x 2048 in groups of 128: 16 waves 62, eight with two blocks each 73; 20000 x 1500: 18.1, 20.5
+            if (blocks <= 16) return f(Shape<DT, 4, 1, 1, 16, 1>());
+            // 256 tokens, 20000 x 4096: 97, 16 waves 105, two tiles of tokens 115
+            return f(Shape<DT, 4, 2, 2, 8, 1>());
+        }
         // 64 tokens, 4096 x 4096: 16 waves and a tile at a time, which take rows whole, 10.2, two tiles in two parts 13.7, of 8 waves 14.5
         // (24 tokens, 50000 x 4096: 53, as the weights pass twice, and two tiles 43)
         if (blocks > 16 && blocks <= 32 && tiles < 1024) return f(Shape<DT, 1, 2, 2, 16, 1>());

@@ -167,3 +167,11 @@ def test_as_many_tokens_and_as_long_a_row_as_there_may_be(dtype):
     for at, value in ((0, 1.0), (1023, 2.0), (1024, 4.0), ((1 << 24) + 1, 8.0), ((1 << 25) - 1, 16.0)):
         x[0, at] = value
     assert layer(x).item() == 31.0
+
+
+@pytest.mark.parametrize("m", [33, 48, 49, 64, 70])
+@pytest.mark.parametrize("k,group", [(1300, 64), (2048, 32), (2500, 128)])
+def test_many_rows_and_tokens(m, k, group):
+    codes, scales, bias, layer = _layer(16390, k, group, m + k)
+    x = torch.randn(m, k, generator=torch.Generator().manual_seed(4)).to(torch.bfloat16).cuda()
+    _check(layer(x), x, codes, scales, bias, group, "%dx16390x%d" % (m, k))
