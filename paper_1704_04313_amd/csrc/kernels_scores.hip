@@ -624,8 +624,9 @@ __device__ void careful_top_lane(const cbinfer_log_probs_args &a, int64_t base, 
 
 // PARTS > 1: the waves of a workgroup share the classes of 256 / PARTS positions, for maps that would not fill the chip
 // otherwise.  CH classes are loaded while those before are worked on.  Bound by memory without alternatives or with few (64 x 8 x 180 x
-// 320 float32, 3 alternatives: 221 MB in 40 us), by the network's instructions with more (10 x 256 x 180 x 320, 590 MB of float32: 122 us
-// without, 156 with 8; bfloat16 79 and 130).
+// 320 float32, 3 alternatives: 221 MB in 39 us), by the network's instructions with more (10 x 256 x 180 x 320, 590 MB of float32: 109 us
+// without, 127 with 8; bfloat16 67 and 110).  Where a class lies is the same for every lane, where a position lies does not change: an
+// address costs no vector instruction (with 64 bits a lane and a bounds check for each: 119, 143, 80 and 132).
 template <int DT, int K, int PARTS>
 __global__ __launch_bounds__(256) void map_kernel(const cbinfer_log_probs_args a, FastDiv inner)
 {
@@ -637,31 +638,46 @@ __global__ __launch_bounds__(256) void map_kernel(const cbinfer_log_probs_args a
     const int part = threadIdx.x / NP, place = threadIdx.x % NP;
     const int64_t pos = (int64_t)blockIdx.x * NP + place;
     const bool there = pos < a.outer * a.inner;
-    const int o = there ? fast_div((int)pos, inner) : 0;
-    const int64_t i = there ? pos - (int64_t)o * a.inner : 0, base = o * a.outer_stride + i * a.inner_stride;
+    const int64_t mine = there ? pos : a.outer * a.inner - 1; // the others read what the last position reads
+    const int o = fast_div((int)mine, inner);
+    const int64_t i = mine - (int64_t)o * a.inner, base = o * a.outer_stride + i * a.inner_stride;
     const Label label = there && part == 0 ? read_label<DT>(a, pos, base) : Label{-1, 0.0f};
     const int n = (int)a.classes, each = (n + PARTS - 1) / PARTS, end = min(n, (part + 1) * each);
-    const T *x = static_cast<const T *>(a.scores) + base + (int64_t)(part * each) * a.class_stride;
+    const int64_t first = (int64_t)blockIdx.x * NP;
+    const int o0 = fast_div((int)first, inner);
+    const int64_t base0 = o0 * a.outer_stride + (first - (int64_t)o0 * a.inner) * a.inner_stride; // of the workgroup's first position
+    const unsigned offset = (unsigned)(base - base0) * (unsigned)sizeof(T); // positions ascend, see run()
+    const int start = __builtin_amdgcn_readfirstlane(part * each);
+    const T *x = static_cast<const T *>(a.scores) + base0 + (int64_t)start * a.class_stride;
     Sums t = {kLowest, 0.0f, 0.0f};
     Ranked best[KK];
 #pragma unroll
     for (int j = 0; j < KK; ++j) best[j] = Ranked::none();
+    const int last_class = __builtin_amdgcn_readfirstlane(end);
     T next[CH];
     const T none = Elem<DT>::put(-__builtin_inff());
     auto load = [&](int c0) {
 #pragma unroll
-        for (int e = 0; e < CH; ++e) next[e] = there && c0 + e < end ? x[e * a.class_stride] : none;
+        for (int e = 0; e < CH; ++e) {
+            // beyond the last class the last again
+            const T *y = x + min(e, last_class - 1 - c0) * a.class_stride;
+            next[e] = *reinterpret_cast<const T *>(reinterpret_cast<const char *>(y) + offset);
+        }
         x += CH * a.class_stride;
+        if (c0 + CH > last_class)
+#pragma unroll
+            for (int e = 0; e < CH; ++e)
+                if (c0 + e >= last_class) next[e] = none;
     };
-    load(part * each);
-    for (int c0 = part * each; c0 < end; c0 += CH) {
+    load(start);
+    for (int c0 = start; c0 < last_class; c0 += CH) {
         float v[CH], most = kLowest;
 #pragma unroll
         for (int e = 0; e < CH; ++e) {
             v[e] = Elem<DT>::get(next[e]);
             most = fmaxf(most, v[e]);
         }
-        load(c0 + CH);
+        if (c0 + CH < last_class) load(c0 + CH);
         raise_to(t, fmaxf(t.m, most));
 #pragma unroll
         for (int e = 0; e < CH; ++e) add(t, v[e]);
@@ -745,10 +761,11 @@ Plan plan(const cbinfer_log_probs_args &a)
         // 64 rows of 100003 bfloat16: 29 us whole, 18 in segments, join included; one of 131071: 28 and 14.
         const int64_t round = 4 * 64 * 4 * (a.dtype == kF32 ? 4 : 8), segments = std::min<int64_t>({(a.classes + round - 1) / round, 64, 1024 / std::max<int64_t>(positions, 1)});
         if (segments >= 4) p.segments = (int)segments;
-    } else if (a.inner_stride == 1 && a.inner >= 16 && a.top <= 16 && (a.classes <= 1024 || positions >= 16384) &&
+    } else if (a.inner_stride == 1 && a.inner >= 16 && (a.outer == 1 || a.outer_stride >= a.inner) && a.top <= 16 && (a.classes <= 1024 || positions >= 16384) &&
                (a.dtype == kF32 || a.classes <= Key<kBF16>::kClasses)) {
         p.kind = kMaps;
-        p.waves = positions < 65536 && a.classes >= 32 ? 4 : 1;
+        // 5 x 191 x 148 x 269 bfloat16, 3 alternatives: a wave each 35 us, four waves 29; float32 without: 28, 33
+        p.waves = positions < (a.top ? 262144 : 65536) && a.classes >= 32 ? 4 : 1;
     }
     return p;
 }
@@ -760,7 +777,24 @@ hipError_t run(hipStream_t st, const cbinfer_log_probs_args &a)
 {
     const Plan p = plan(a);
     const int64_t positions = a.outer * a.inner;
-    if (p.kind == kMaps) return p.waves == 4 ? map_any<DT, 4>(st, a) : map_any<DT, 1>(st, a);
+    if (p.kind == kMaps) {
+        const auto maps = [&](const cbinfer_log_probs_args &b) { return p.waves == 4 ? map_any<DT, 4>(st, b) : map_any<DT, 1>(st, b); };
+        // offsets from a workgroup's first position have 32 bits
+        const int64_t e = sizeof(typename Elem<DT>::type);
+        if (a.outer == 1 || a.outer_stride < (((int64_t)1 << 32) / e - 256) / (255 / a.inner + 2)) return maps(a);
+        for (int64_t o = 0; o < a.outer; ++o) { // maps of gigabytes, one at a time
+            cbinfer_log_probs_args b = a;
+            b.outer = 1;
+            b.scores = static_cast<const typename Elem<DT>::type *>(a.scores) + o * a.outer_stride;
+            if (a.labels) b.labels = static_cast<const char *>(a.labels) + o * a.inner * a.label_bytes;
+            if (a.label) b.label = a.label + o * a.inner;
+            if (a.entropy) b.entropy = a.entropy + o * a.inner;
+            if (a.top_values) b.top_values = a.top_values + o * a.top * a.inner;
+            if (a.top_index) b.top_index = a.top_index + o * a.top * a.inner;
+            if (hipError_t err = maps(b)) return err;
+        }
+        return hipSuccess;
+    }
     constexpr int U = DT == kF32 ? 4 : 2;
     float *found = static_cast<float *>(a.workspace);
     const FastDiv inner = make_fastdiv((int)a.inner);

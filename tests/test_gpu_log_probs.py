@@ -151,3 +151,29 @@ def test_nothing_to_do_and_other_streams():
     torch.cuda.current_stream().wait_stream(side)
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("outer_stride", [0, 7, 640, 1300])
+def test_maps_that_overlap_or_repeat(outer_stride, dtype):
+    x = _scores((6000,), dtype, 9).as_strided((5, 40, 16), (outer_stride, 16, 1))
+    labels = _labels((5, 16), 40, 4)
+    check_log_probs(cb.log_probs(x, labels, top=5), x, labels, 1, 5, "stride %d" % outer_stride)
+
+
+@pytest.mark.parametrize("dtype,outer_stride", [(torch.float32, 1 << 26), (torch.bfloat16, 1 << 27)])
+@pytest.mark.parametrize("inner", [16, 300])
+def test_maps_far_apart(dtype, outer_stride, inner):
+    """A workgroup's positions span more than 32 bits of offsets, were the maps as many as it has positions for."""
+    memory = torch.empty(2 * outer_stride + 100 * inner, dtype=dtype, device="cuda")
+    x = memory.as_strided((3, 37, inner), (outer_stride, inner, 1))
+    x.copy_(_scores((3, 37, inner), dtype, inner))
+    labels = _labels((3, inner), 37, 8)
+    check_log_probs(cb.log_probs(x, labels, top=4), x, labels, 1, 4, "far apart")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,classes,h,w,top", [(1, 33, 20, 20, 3), (2, 35, 16, 31, 5), (3, 47, 40, 40, 1), (2, 9, 250, 260, 2), (5, 40, 230, 235, 3)])
+def test_maps_shared_by_waves(n, classes, h, w, top, dtype):
+    x, l = _scores((n, classes, h, w), dtype, classes), _labels((n, h, w), classes, n, torch.int32)
+    check_log_probs(cb.log_probs(x, l, top=top), x, l, 1, top, "map")
