@@ -173,7 +173,14 @@ def test_maps_far_apart(dtype, outer_stride, inner):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("n,classes,h,w,top", [(1, 33, 20, 20, 3), (2, 35, 16, 31, 5), (3, 47, 40, 40, 1), (2, 9, 250, 260, 2), (5, 40, 230, 235, 3)])
-def test_maps_shared_by_waves(n, classes, h, w, top, dtype):
+@pytest.mark.parametrize("n,classes,h,w,top", [(1, 33, 20, 20, 3), (2, 35, 16, 31, 5), (3, 47, 40, 40, 1), (2, 9, 250, 260, 2), (5, 40, 230, 235, 3),
+                                               (5, 40, 230, 235, 0)])
+def test_larger_maps(n, classes, h, w, top, dtype):
+    """A waves' share of the classes, or all of them a lane: some of the positions."""
     x, l = _scores((n, classes, h, w), dtype, classes), _labels((n, h, w), classes, n, torch.int32)
-    check_log_probs(cb.log_probs(x, l, top=top), x, l, 1, top, "map")
+    got = cb.log_probs(x, l, top=top)
+    some = torch.randint(0, n * h * w, (200,), generator=torch.Generator().manual_seed(top)).cuda()
+    some[0], some[1] = 0, n * h * w - 1
+    rows = lambda t: t.movedim(1, -1).flatten(0, 2)[some]  # noqa: E731
+    got = type(got)(got.label.flatten()[some], got.entropy.flatten()[some], rows(got.top) if top else None, rows(got.index) if top else None)
+    check_log_probs(got, rows(x), l.flatten()[some], 1, top, "map")
