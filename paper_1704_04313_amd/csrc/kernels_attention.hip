@@ -235,10 +235,12 @@ __device__ __forceinline__ int swizzle_across(int row)
 struct Keys {
     int64_t state; // from a head's state to the next
     bool add;
+    bool fold; // the outputs' kernel joins the parts itself
 };
 
 // OUT: outputs of the tokens of a part (`per` chunks) of the sequence, from the state in front of it.  Otherwise what those
-// tokens leave in a state of zero, where further tokens follow.  `states`: [stream][head][part][key_size][value_size].
+// tokens leave in a state of zero, the first part's in the state that is there, where further tokens follow.  `states`:
+// [stream][head][part][key_size][value_size], first the state that was there, then what part 0, 1, ... leaves.
 // WHOLE: rows are pieces of 16 bytes at 16-byte addresses.
 template <int DT, int KT, int NC, bool OUT, bool WHOLE>
 __global__ __launch_bounds__(NC * 128, NC == 4 || DT == kBF16 ? 2 : 1) void chunk_kernel(const cbinfer_linear_attention_args a, int slices, int per, int parts, float *states, Keys keys)
@@ -329,12 +331,32 @@ __global__ __launch_bounds__(NC * 128, NC == 4 || DT == kBF16 ? 2 : 1) void chun
     auto place = [&](int kt, int r) { return state_at + (unsigned)((32 * kt + 8 * (r / 4) + r % 4) * dv) * 4; };
     f32x16 S[KH] = {};
     float *state = a.state + bh * keys.state;
-    if (OUT) {
-        const Buffer from = buffer(parts > 1 ? states + ((int64_t)bh * parts + part) * dk * dv : state, state_bytes);
+    const int64_t size = (int64_t)dk * dv;
+    states += bh * parts * size;
+    if (OUT || part == 0) {
+        const bool whole = !OUT || n <= per * kChunk; // nobody else writes the state, or only later
+        const Buffer from = buffer(whole ? state : states + (keys.fold ? min(part, 1) : part) * size, state_bytes), first = buffer(states, state_bytes);
 #pragma unroll
         for (int kt = 0; kt < KH; ++kt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) S[kt][r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(from, place(kt, r), 0, 0));
+        if (!OUT) {
+#pragma unroll
+            for (int kt = 0; kt < KH; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S[kt][r]), first, place(kt, r), 0, 0);
+        }
+    }
+    if (OUT && keys.fold) {
+        const float through = power(g, per * kChunk);
+        for (int p = 2; p <= part; ++p) {
+            const Buffer from = buffer(states + p * size, state_bytes);
+#pragma unroll
+            for (int kt = 0; kt < KH; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    S[kt][r] = __builtin_fmaf(through, S[kt][r], __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(from, place(kt, r), 0, 0)));
+        }
     }
 
     int turn = 0;
@@ -575,7 +597,7 @@ __global__ __launch_bounds__(NC * 128, NC == 4 || DT == kBF16 ? 2 : 1) void chun
     }
 
     if (!OUT || t1 == n) { // the part with the last token
-        const Buffer to = buffer(OUT ? state : states + ((int64_t)bh * parts + part + 1) * dk * dv, state_bytes);
+        const Buffer to = buffer(OUT ? state : states + (part + 1) * size, state_bytes);
 #pragma unroll
         for (int kt = 0; kt < KH; ++kt)
 #pragma unroll
@@ -583,18 +605,18 @@ __global__ __launch_bounds__(NC * 128, NC == 4 || DT == kBF16 ? 2 : 1) void chun
     }
 }
 
-// What the parts of a sequence leave by themselves (places 1, 2, ...) becomes the states in front of the parts.  Bound by memory:
-// 16 heads of 128 x 128 in 16 parts, 33 MB, 8 us.
-__global__ __launch_bounds__(256) void join_parts_kernel(const cbinfer_linear_attention_args a, int per, int parts, float *states, Keys keys)
+// What the parts of a sequence leave (places 1, 2, ...) becomes the states in front of the parts.  Bound by memory: 16 heads of
+// 128 x 128 in 16 parts, 33 MB, 8 us.
+__global__ __launch_bounds__(256) void join_parts_kernel(const cbinfer_linear_attention_args a, int per, int parts, float *states)
 {
     const int bh = blockIdx.y, size = a.key_size * a.value_size, at = blockIdx.x * 256 + threadIdx.x, b = bh / a.heads;
     if (at >= size) return;
     const int n = a.lengths ? min(max(a.lengths[b], 0), a.tokens) : a.tokens;
-    const float g = power(a.decay[bh - b * a.heads], per * kChunk);
-    float *s = states + (int64_t)bh * parts * size + at, x = a.state[bh * keys.state + at];
     const int last = (int)min((int64_t)parts, ((int64_t)n + per * kChunk - 1) / (per * kChunk)); // parts with tokens
-    s[0] = x;
-    for (int p0 = 1; p0 < last; p0 += 8) { // eight loads on their way at a time
+    if (last <= 2) return;
+    const float g = power(a.decay[bh - b * a.heads], per * kChunk);
+    float *s = states + (int64_t)bh * parts * size + at, x = s[size];
+    for (int p0 = 2; p0 < last; p0 += 8) { // eight loads on their way at a time
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = p0 + i < last ? s[(int64_t)(p0 + i) * size] : 0.0f;
@@ -628,14 +650,11 @@ Plan plan(const cbinfer_linear_attention_args &a)
     // float32: 3 parts 83, 6 62, 7 70, 8 64).  Of two tiles in bfloat16 a compute unit takes two workgroups (6 streams of 1749 tokens, 12 heads
     // of 96 x 64: 52, with one 67).
     const int64_t room = (a.lengths ? 400 : 256) * (p.tiles == 2 && a.dtype == kBF16 ? 2 : 1);
-    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(chunks, room / std::max<int64_t>(groups, 1)));
-    // Whether they pay, in us as measured: a chunk takes `each`, and 0.7 of it again in a part; two more launches 8, a state 8 bytes a value
-    // at 4.5 TB/s.  8 streams of 600 tokens, 16 heads of 128 x 128: 45, in two parts 62; 16 of 500 tokens, 16 of 64 x 64: 28, 39; 4 of 1000
-    // tokens, 16 of 128 x 128: 63, in four 48; one of 147 tokens, 2 heads, float32: 34, in three 24.
-    const float each = a.dtype == kF32 ? (a.key_size > 64 ? 11.0f : 7.5f) : a.key_size > 128 ? 8.0f : p.tiles == 4 ? 4.3f : a.key_size > 64 ? 3.6f : 2.9f;
-    const float side = groups * p.parts > 256 && room > 400 ? 0.7f * p.parts : p.parts; // by side: the second workgroup of a unit is worth less
-    const float gain = chunks * each * (1.0f - 1.7f / side) * (a.lengths ? 0.75f : 1.0f);
-    if (gain < 8.0f + heads * p.parts * (float)a.key_size * a.value_size * 8.0f / 4.5e6f) p.parts = 1;
+    // From 256 on they do not pay (16 streams of up to 500 tokens, 16 heads of 64 x 64: 28, in three parts 33); below, already with three chunks
+    // (2 streams of 190 tokens, 16 heads of 128 x 128: 15.1, in three parts 13.7; two chunks, 2 streams of 100, 4 heads of 64 x 64: 9.2, 11.6), in
+    // float32 with two (4 streams of 100 tokens, 4 heads of 64 x 128: 18.6, 17.0).
+    const bool pays = groups < 256 && chunks > (a.dtype == kF32 ? 1 : 2);
+    p.parts = pays ? (int)std::max<int64_t>(1, std::min(chunks, room / std::max<int64_t>(groups, 1))) : 1;
     p.per = (int)((chunks + p.parts - 1) / p.parts);
     p.parts = (int)((chunks + p.per - 1) / p.per);
     return p;
@@ -649,27 +668,30 @@ hipError_t chunked(hipStream_t st, const cbinfer_linear_attention_args &a, const
     if (p.parts > 1) {
         chunk_kernel<DT, KT, NC, false, WHOLE><<<dim3(groups, p.parts - 1), NC * 128, 0, st>>>(a, p.slices, p.per, p.parts, states, keys);
         if (hipError_t err = hipGetLastError()) return err;
-        join_parts_kernel<<<dim3((a.key_size * a.value_size + 255) / 256, a.streams * a.heads), 256, 0, st>>>(a, p.per, p.parts, states, keys);
-        if (hipError_t err = hipGetLastError()) return err;
+        if (!keys.fold) {
+            join_parts_kernel<<<dim3((a.key_size * a.value_size + 255) / 256, a.streams * a.heads), 256, 0, st>>>(a, p.per, p.parts, states);
+            if (hipError_t err = hipGetLastError()) return err;
+        }
     }
     chunk_kernel<DT, KT, NC, true, WHOLE><<<dim3(groups, p.parts), NC * 128, 0, st>>>(a, p.slices, p.per, p.parts, states, keys);
     return hipGetLastError();
 }
 
 constexpr int kKeys = 128; // at a time, float32
+constexpr int kFold = 16; // parts up to which the outputs' kernel joins them: 4 streams of 1000 tokens, 16 heads of 128 x 128, 4 parts: 39 us, joined before 49; one of 8192, 16 parts: 72, 76
 
 template <int DT, bool WHOLE>
 hipError_t chunked_any(hipStream_t st, const cbinfer_linear_attention_args &a, const Plan &p)
 {
     if constexpr (DT == kBF16)
-        if (a.key_size > 128) return chunked<DT, 8, 4, WHOLE>(st, a, p, {(int64_t)a.key_size * a.value_size, false});
+        if (a.key_size > 128) return chunked<DT, 8, 4, WHOLE>(st, a, p, {(int64_t)a.key_size * a.value_size, false, p.parts <= kFold});
     for (int k0 = 0; k0 < a.key_size; k0 += kKeys) { // once but for float32 keys of more than 128
         cbinfer_linear_attention_args b = a;
         b.key_size = std::min(a.key_size - k0, kKeys);
         b.q = static_cast<const typename Elem<DT>::type *>(a.q) + k0;
         b.k = static_cast<const typename Elem<DT>::type *>(a.k) + k0;
         b.state = a.state + (int64_t)k0 * a.value_size;
-        const Keys keys = {(int64_t)a.key_size * a.value_size, k0 > 0};
+        const Keys keys = {(int64_t)a.key_size * a.value_size, k0 > 0, p.parts <= kFold};
         const hipError_t err = b.key_size <= 64 ? p.tiles == 2 ? chunked<DT, 2, 2, WHOLE>(st, b, p, keys) : chunked<DT, 2, 4, WHOLE>(st, b, p, keys)
                                                 : p.tiles == 2 ? chunked<DT, 4, 2, WHOLE>(st, b, p, keys) : chunked<DT, 4, 4, WHOLE>(st, b, p, keys);
         if (err) return err;
