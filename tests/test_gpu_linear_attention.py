@@ -150,3 +150,10 @@ def test_output_given_and_no_tokens():
 def test_prompts_with_long_keys(dk, dv, dtype):
     _run(1, 400, 3, 1, dk, dv, dtype, what="long keys")
     _run(4, 300, 2, 2, dk, dv, dtype, lengths=[300, 0, 64, 131], what="long keys, ragged")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_more_parts_than_an_output_joins(dtype):
+    _run(1, 1500, 1, 1, 64, 48, dtype, what="many parts")
+    _run(2, 1300, 1, 1, 160, 32, dtype, lengths=[1300, 700], what="many parts, ragged")
+    _run(3, 1100, 1, 1, 32, 32, dtype, lengths=[64, 65, 1088], what="a chunk, and one token more")
