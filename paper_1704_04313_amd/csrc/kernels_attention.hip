@@ -130,8 +130,8 @@ hipError_t recurrent_any(hipStream_t st, const cbinfer_linear_attention_args &a)
 //
 // A workgroup of eight waves takes 5 us for 64 tokens and a state of 128 x 128 in bfloat16: 1.4 us of matrix instructions, 2 of other
 // vector instructions (splitting values most of all), three barriers, and the two waves of a SIMD hardly overlap the two kinds.
-// 8192 tokens of 16 such heads: outputs 46 us for 134 MB (28 with no arithmetic, 39 with no loads and stores), before that what the
-// parts leave 22, which its loads take too, and the joining of the parts 8.
+// 8192 tokens of 16 such heads: outputs 51 us for 134 MB, the joining of 16 parts among them (without it 46; 28 with no arithmetic, 39 with
+// no loads and stores), before that what the parts leave 22, which its loads take too.
 //
 // bfloat16: what is computed on the way enters a product as a sum of bfloat16 -- scores and states two (16 bits are kept;
 // the output keeps 8), the faded values, from which the state is added up, three (24 bits, exact).  float32: the float32
