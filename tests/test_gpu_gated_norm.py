@@ -131,3 +131,10 @@ def test_rows_that_end_inside_eight(rows, d, kind, sum_kind):
     t = _all(rows, d, kind, sum_kind)
     kw = dict(weight=t["weight"], gate=t["gate"], activation="sigmoid", residual=t["residual"], scale=t["channel"], next_weight=t["next"])
     _check(*cb.gated_norm(t["x"], **kw), t["x"], "%dx%d" % (rows, d), **kw)
+
+
+@pytest.mark.parametrize("kind,sum_kind", KINDS)
+def test_no_rows(kind, sum_kind):
+    x, w = torch.empty(0, 24, dtype=kind, device="cuda"), torch.ones(24, device="cuda")
+    h, y = cb.gated_norm(x, w, group=8, residual=torch.empty(0, 24, dtype=sum_kind, device="cuda"), next_weight=w)
+    assert h.shape == y.shape == (0, 24) and h.dtype == sum_kind and y.dtype == kind

@@ -175,3 +175,10 @@ def test_many_rows_and_tokens(m, k, group):
     codes, scales, bias, layer = _layer(16390, k, group, m + k)
     x = torch.randn(m, k, generator=torch.Generator().manual_seed(4)).to(torch.bfloat16).cuda()
     _check(layer(x), x, codes, scales, bias, group, "%dx16390x%d" % (m, k))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_no_tokens(dtype):
+    layer = _layer(40, 70, 32, 1)[3]
+    assert layer(torch.empty(0, 70, dtype=dtype, device="cuda")).shape == (0, 40)
+    assert layer(torch.empty(2, 0, 3, 70, dtype=dtype, device="cuda")).shape == (2, 0, 3, 40)
