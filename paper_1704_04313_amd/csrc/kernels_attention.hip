@@ -10,7 +10,7 @@ namespace {
 
 // Token after token, the state in registers.  A workgroup holds `columns` columns of one stream's head: DVL lanes side by
 // side, VEC columns each, and 256 / DVL groups of lanes that share the rows (RPT each).  Bound by the state's way through memory
-// where tokens are few (they are until 16, see plan()): it is read and written once, 128 bytes of a row by 8 lanes.  64 streams of 16 heads of 128 x 128, one token:
+// where tokens are few (see plan()): it is read and written once, 128 bytes of a row by 8 lanes.  64 streams of 16 heads of 128 x 128, one token:
 // 25 us for 135 MB, 5.4 TB/s; where rows of the state are not whole pieces of 16 bytes (128 x 127), a column a lane, 40.
 template <int DT, int VEC, int DVL, int RPT>
 __global__ __launch_bounds__(256) void recurrent_kernel(const cbinfer_linear_attention_args a, int slices)
@@ -636,7 +636,9 @@ struct Plan {
 Plan plan(const cbinfer_linear_attention_args &a)
 {
     Plan p = {false, 1, 1, 1, 4};
-    if (a.tokens < 16) return p;
+    // us for 64 streams, 16 heads of 128 x 128, token after token and in chunks: bfloat16 4 tokens 36, 37, 6 tokens 44, 36, 15 tokens 77, 37; float32 12
+    // tokens 57, 75; 16 streams, 8 heads, float32 15 tokens: 19, 17.
+    if (a.tokens < (a.dtype == kF32 ? 16 : 5)) return p;
     p.chunks = true;
     const int tiles = (a.value_size + 31) / 32;
     const int64_t heads = (int64_t)a.streams * a.heads, chunks = (a.tokens + kChunk - 1) / kChunk;
