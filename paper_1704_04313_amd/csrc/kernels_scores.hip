@@ -642,7 +642,8 @@ __global__ __launch_bounds__(256) void map_kernel(const cbinfer_log_probs_args a
     const int o = fast_div((int)mine, inner);
     const int64_t i = mine - (int64_t)o * a.inner, base = o * a.outer_stride + i * a.inner_stride;
     const Label label = there && part == 0 ? read_label<DT>(a, pos, base) : Label{-1, 0.0f};
-    const int n = (int)a.classes, each = (n + PARTS - 1) / PARTS, end = min(n, (part + 1) * each);
+    // Whole rounds of CH: what a round has beyond `end` is a score of -inf at the next classes' numbers, which must not be those of another part
+    const int n = (int)a.classes, each = PARTS == 1 ? n : ((n + PARTS - 1) / PARTS + CH - 1) / CH * CH, end = min(n, (part + 1) * each);
     const int64_t first = (int64_t)blockIdx.x * NP;
     const int o0 = fast_div((int)first, inner);
     const int64_t base0 = o0 * a.outer_stride + (first - (int64_t)o0 * a.inner) * a.inner_stride; // of the workgroup's first position
@@ -659,7 +660,7 @@ __global__ __launch_bounds__(256) void map_kernel(const cbinfer_log_probs_args a
     auto load = [&](int c0) {
 #pragma unroll
         for (int e = 0; e < CH; ++e) {
-            // beyond the last class the last again
+            // beyond the last class the last again, also where a part has none
             const T *y = x + min(e, last_class - 1 - c0) * a.class_stride;
             next[e] = *reinterpret_cast<const T *>(reinterpret_cast<const char *>(y) + offset);
         }

@@ -184,3 +184,19 @@ def test_larger_maps(n, classes, h, w, top, dtype):
     rows = lambda t: t.movedim(1, -1).flatten(0, 2)[some]  # noqa: E731
     got = type(got)(got.label.flatten()[some], got.entropy.flatten()[some], rows(got.top) if top else None, rows(got.index) if top else None)
     check_log_probs(got, rows(x), l.flatten()[some], 1, top, "map")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("classes", [32, 33, 36, 40, 47, 56, 61])
+@pytest.mark.parametrize("top", [8, 10, 12, 16])
+def test_maps_with_fewer_live_classes_than_alternatives(classes, top, dtype):
+    """Positions with 0 .. top - 1 classes that are not ruled out, anywhere among the classes: those ruled out follow, each once, the
+    lowest first, wherever a position's classes are divided among waves."""
+    g = torch.Generator().manual_seed(classes + 100 * top)
+    x = torch.randn(2, classes, 6, 16, generator=g)
+    places = torch.rand(2, classes, 6, 16, generator=g).argsort(1).argsort(1)
+    live = (torch.arange(2 * 6 * 16) % top).view(2, 1, 6, 16)
+    x[places >= live] = float("-inf")
+    x = x.to(dtype).cuda()
+    labels = _labels((2, 6, 16), classes, top)
+    check_log_probs(cb.log_probs(x, labels, top=top), x, labels, 1, top, "%d classes, %d best" % (classes, top))
