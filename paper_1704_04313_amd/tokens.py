@@ -248,6 +248,15 @@ def log_probs(scores, labels=None, *, dim: int = 1, top: int = 0) -> LogProbs:
     return LogProbs(label, entropy, values, index)
 
 
+class _LayerPlan(NamedTuple):
+    """What a layer's call needs besides addresses.  Made whole and kept in one assignment, read in one: calls of other threads
+    may come in between."""
+    geometry: tuple
+    args: C.Structure
+    shape: tuple
+    workspace: int
+
+
 # ---- linear attention ---------------------------------------------------------------------------
 class LinearAttention:
     """Linear attention with a decay for each head, and the states of `n_streams` streams.
@@ -273,7 +282,7 @@ class LinearAttention:
         self.decay = torch.tensor(decay, dtype=torch.float32).cuda()
         self._state = torch.zeros((self.n_streams, self.heads, self.key_size, self.value_size), dtype=torch.float32,
                                   device=self.decay.device)
-        self._geometry = None
+        self._plan: Optional[_LayerPlan] = None
         a = self._args = linear_attention_args()
         a.streams, a.heads, a.kv_heads = self.n_streams, self.heads, self.kv_heads
         a.key_size, a.value_size, a.scale = self.key_size, self.value_size, self.scale
@@ -293,19 +302,19 @@ class LinearAttention:
         v [..][kv_heads][value_size], the last axis contiguous; lengths: None, or int32 [n_streams], how many of the
         tokens a stream has.  Returns [n_streams][tokens][heads][value_size] and leaves the new state."""
         geometry = (q.shape, q.stride(), k.shape, k.stride(), v.shape, v.stride(), q.dtype, k.dtype, v.dtype, lengths is None)
-        if geometry != self._geometry:
-            self._plan(q, k, v, lengths)
-            self._geometry = geometry
-        a = linear_attention_args.from_buffer_copy(self._args)
+        plan = self._plan
+        if plan is None or plan.geometry != geometry:
+            plan = self._plan = self._planned(geometry, q, k, v, lengths)
+        a = linear_attention_args.from_buffer_copy(plan.args)
         device = _device(q, "q")
         _same_device(k, device, "k")
         _same_device(v, device, "v")
         _same_device(self._state, device, "the state")
         if out is None:
-            out = torch.empty(self._shape, dtype=q.dtype, device=device)
+            out = torch.empty(plan.shape, dtype=q.dtype, device=device)
         else:
-            if out.shape != self._shape or out.dtype != q.dtype or out.device != device or (self.value_size > 1 and out.stride(3) != 1):
-                _refuse("out must be a tensor like q of shape %s" % (self._shape,))
+            if out.shape != plan.shape or out.dtype != q.dtype or out.device != device or (self.value_size > 1 and out.stride(3) != 1):
+                _refuse("out must be a tensor like q of shape %s" % (plan.shape,))
             a.o_stride[:] = out.stride()[:3]
         if lengths is not None:
             if lengths.dtype != torch.int32 or lengths.shape != (self.n_streams,) or not lengths.is_contiguous():
@@ -313,16 +322,15 @@ class LinearAttention:
             _same_device(lengths, device, "lengths")
             a.lengths = lengths.data_ptr()
         a.q, a.k, a.v, a.o = q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr()
-        keep = _workspace(a, self._workspace_bytes, device)  # noqa: F841
+        keep = _workspace(a, plan.workspace, device)  # noqa: F841
         rc = self.lib.cbinfer_linear_attention(a, _stream(device))
         if rc:
             _raise(rc)
         return out
 
-    def _plan(self, q, k, v, lengths):
+    def _planned(self, geometry, q, k, v, lengths) -> _LayerPlan:
         """Checks of shapes and types, and what follows from them; kept for calls of the same geometry."""
-        self._geometry = None
-        a = self._args
+        a = linear_attention_args.from_buffer_copy(self._args)
         if q.dim() != 4:
             _refuse("q must be [streams][tokens][heads][key_size]")
         tokens = q.shape[1]
@@ -336,11 +344,11 @@ class LinearAttention:
                 _refuse("%s: the last axis must be contiguous" % what)
         a.dtype = _dtype(q, "q")
         a.tokens = tokens
-        self._shape = (self.n_streams, tokens, self.heads, self.value_size)
         a.q_stride[:], a.k_stride[:], a.v_stride[:] = q.stride()[:3], k.stride()[:3], v.stride()[:3]
         a.o_stride[:] = (tokens * self.heads * self.value_size, self.heads * self.value_size, self.value_size)
         a.lengths = None if lengths is None else a.state  # of the workspace it matters only whether there are any
-        self._workspace_bytes = self.lib.cbinfer_linear_attention_workspace_bytes(a)
+        return _LayerPlan(geometry, a, (self.n_streams, tokens, self.heads, self.value_size),
+                          self.lib.cbinfer_linear_attention_workspace_bytes(a))
 
 
 # ---- products with 4-bit weights ------------------------------------------------------------------
@@ -390,7 +398,7 @@ class QuantisedLinear:
         rc = self.lib.cbinfer_pack_weights(codes.data_ptr(), scales.data_ptr(), self.rows, self.cols, self.group, packed, _stream(device))
         if rc:
             _raise(rc)
-        self._geometry = None
+        self._plan: Optional[_LayerPlan] = None
         a = self._args = quantised_product_args()
         a.group, a.rows, a.cols, a.packed = self.group, self.rows, self.cols, packed
         a.bias = None if bias is None else bias.data_ptr()
@@ -403,36 +411,34 @@ class QuantisedLinear:
     def __call__(self, x, out=None):
         """x [..][cols] float32 or bfloat16 -> [..][rows] of the same type.  Rows of x may lie apart, not their values."""
         geometry = (x.shape, x.stride(), x.dtype)
-        if geometry != self._geometry:
-            self._plan(x)
-            self._geometry = geometry
-        a = quantised_product_args.from_buffer_copy(self._args)
+        plan = self._plan
+        if plan is None or plan.geometry != geometry:
+            plan = self._plan = self._planned(geometry, x)
+        a = quantised_product_args.from_buffer_copy(plan.args)
         device = _device(x, "x")
         _same_device(self._memory, device, "the layer")
         if out is None:
-            out = torch.empty(self._shape, dtype=x.dtype, device=device)
-        elif out.shape != self._shape or out.dtype != x.dtype or out.device != device or not out.is_contiguous():
-            _refuse("out must be a contiguous tensor like x of shape %s" % (tuple(self._shape),))
+            out = torch.empty(plan.shape, dtype=x.dtype, device=device)
+        elif out.shape != plan.shape or out.dtype != x.dtype or out.device != device or not out.is_contiguous():
+            _refuse("out must be a contiguous tensor like x of shape %s" % (tuple(plan.shape),))
         a.x, a.y = x.data_ptr(), out.data_ptr()
-        keep = _workspace(a, self._workspace_bytes, device)  # noqa: F841
+        keep = _workspace(a, plan.workspace, device)  # noqa: F841
         rc = self.lib.cbinfer_quantised_product(a, _stream(device))
         if rc:
             _raise(rc)
         return out
 
-    def _plan(self, x):
+    def _planned(self, geometry, x) -> _LayerPlan:
         """Checks of shape and type, and what follows from them; kept for calls of the same geometry."""
-        self._geometry = None
-        a = self._args
+        a = quantised_product_args.from_buffer_copy(self._args)
         if x.dim() < 1 or x.shape[-1] != self.cols:
             _refuse("x must end in an axis of %d values (got %s)" % (self.cols, tuple(x.shape)))
         if self.cols > 1 and x.stride(-1) != 1:
             _refuse("x: the last axis must be contiguous")
         a.dtype = _dtype(x, "x")
-        self._shape = x.shape[:-1] + (self.rows,)
         a.tokens, a.x_stride = _joined_rows(x)
         a.y_stride = self.rows
-        self._workspace_bytes = self.lib.cbinfer_quantised_product_workspace_bytes(a)
+        return _LayerPlan(geometry, a, x.shape[:-1] + (self.rows,), self.lib.cbinfer_quantised_product_workspace_bytes(a))
 
 
 def _joined_rows(t):

@@ -1,5 +1,7 @@
 """Products with 4-bit weights against 64 bits: every code, sizes that end inside a group, a block and a tile, strides,
 values that are not finite."""
+import threading
+
 import pytest
 import torch
 
@@ -182,3 +184,25 @@ def test_no_tokens(dtype):
     layer = _layer(40, 70, 32, 1)[3]
     assert layer(torch.empty(0, 70, dtype=dtype, device="cuda")).shape == (0, 40)
     assert layer(torch.empty(2, 0, 3, 70, dtype=dtype, device="cuda")).shape == (2, 0, 3, 40)
+
+
+def test_a_layer_used_by_two_threads():
+    """Each with its own tokens, on its own stream, at the same time: what each gets alone."""
+    layer = _layer(300, 9000, 64, 9)[3]
+    work = [torch.randn(m, 9000, generator=torch.Generator().manual_seed(m)).to(t).cuda() for m, t in ((3, torch.float32), (70, torch.bfloat16))]
+    alone = [layer(x) for x in work]
+    torch.cuda.synchronize()
+    got = [[], []]
+
+    def call(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(200):
+                got[i].append(layer(work[i]))
+            torch.cuda.current_stream().synchronize()
+    threads = [threading.Thread(target=call, args=(i,)) for i in (0, 1)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for i in (0, 1):
+        assert len(got[i]) == 200 and all(torch.equal(y, alone[i]) for y in got[i])

@@ -3,6 +3,7 @@ before it touches the device, and so do the Python entry points."""
 import ctypes as C
 import os
 import re
+import threading
 
 import pytest
 import torch
@@ -162,3 +163,88 @@ def test_python_entry_points_refuse():
             call()
     att.process(q, k, k)  # and what is right still runs
     layer(x)
+
+
+class _Recorder:
+    """The library without its launches: the arguments of every call are kept instead, and what shall happen while a layer looks
+    at its tensors or asks for its workspace, as another thread may run there, happens once."""
+
+    def __init__(self, lib):
+        self.lib, self.calls, self.meanwhile = lib, [], None
+
+    def pause(self):
+        what, self.meanwhile = self.meanwhile, None
+        if what:
+            thread = threading.Thread(target=what)
+            thread.start()
+            thread.join()
+
+    def __getattr__(self, name):
+        if name.endswith("_workspace_bytes"):
+            def sizes(a):
+                self.pause()
+                return getattr(self.lib, name)(a)
+            return sizes
+        if name in ("cbinfer_quantised_product", "cbinfer_linear_attention"):
+            def launch(a, stream):
+                self.calls.append(a)
+                return 0
+            return launch
+        if name in ("cbinfer_pack_weights", "cbinfer_quantise_weights"):
+            return lambda *args: 0
+        return getattr(self.lib, name)
+
+
+@pytest.fixture
+def recorder(monkeypatch):
+    r = _Recorder(tokens._library())
+    monkeypatch.setattr(tokens, "_library", lambda: r)
+    monkeypatch.setattr(tokens, "_device", lambda t, what: (r.pause(), t.device)[1])
+    monkeypatch.setattr(tokens, "_stream", lambda device: 0)
+    monkeypatch.setattr(torch.cuda, "is_available", lambda: True)
+    monkeypatch.setattr(torch.Tensor, "cuda", lambda t: t)
+    return r
+
+
+@pytest.mark.parametrize("first", [(3, 64), (64, 3)])
+@pytest.mark.parametrize("dtypes", [(torch.float32, torch.float32), (torch.float32, torch.bfloat16)])
+def test_a_layer_called_by_two_threads(recorder, first, dtypes):
+    """A call made in the middle of another one, with other tokens, changes nothing about it, nor about later calls."""
+    layer = cb.QuantisedLinear(torch.zeros(40, 9000, dtype=torch.uint8), torch.zeros(40, 141, dtype=torch.bfloat16))
+    x, z = (torch.zeros(n, 9000, dtype=t) for n, t in zip(first, dtypes))
+    made = {}
+
+    def call(t):
+        made[t.data_ptr()] = layer(t)
+    for turn in range(4):
+        recorder.calls.clear()
+        recorder.meanwhile = lambda: call(z)
+        call(x)
+        assert len(recorder.calls) == 2
+        for a in recorder.calls:
+            t = x if a.x == x.data_ptr() else z
+            out = made[t.data_ptr()]
+            assert (a.tokens, a.x, a.y, a.dtype) == (t.shape[0], t.data_ptr(), out.data_ptr(), 0 if t.dtype == torch.float32 else 1)
+            assert out.shape == (t.shape[0], 40) and out.dtype == t.dtype
+            assert a.workspace_bytes >= recorder.lib.cbinfer_quantised_product_workspace_bytes(a) > 0
+
+
+@pytest.mark.parametrize("first", [(1, 500), (500, 1), (300, 200)])
+def test_attention_called_by_two_threads(recorder, first):
+    att = cb.LinearAttention([0.9, 0.8], 16, 32)
+    some = [(torch.zeros(1, n, 2, 16), torch.zeros(1, n, 2, 16), torch.zeros(1, n, 2, 32)) for n in first]
+    made = {}
+
+    def call(qkv):
+        made[qkv[0].data_ptr()] = att.process(*qkv)
+    for turn in range(4):
+        recorder.calls.clear()
+        recorder.meanwhile = lambda: call(some[1])
+        call(some[0])
+        assert len(recorder.calls) == 2
+        for a in recorder.calls:
+            q = next(t[0] for t in some if t[0].data_ptr() == a.q)
+            out = made[a.q]
+            assert (a.tokens, a.o) == (q.shape[1], out.data_ptr()) and out.shape == (1, q.shape[1], 2, 32)
+            assert list(a.q_stride) == list(q.stride()[:3]) and list(a.o_stride) == list(out.stride()[:3])
+            assert a.workspace_bytes >= recorder.lib.cbinfer_linear_attention_workspace_bytes(a)
