@@ -133,9 +133,8 @@ hipError_t recurrent_any(hipStream_t st, const cbinfer_linear_attention_args &a)
 // 8192 tokens of 16 such heads: outputs 51 us for 134 MB, the joining of 16 parts among them (without it 46; 28 with no arithmetic, 39 with
 // no loads and stores), before that what the parts leave 22, which its loads take too.
 //
-// bfloat16: what is computed on the way enters a product as a sum of bfloat16 -- scores and states two (16 bits are kept;
-// the output keeps 8), the faded values, from which the state is added up, three (24 bits, exact).  float32: the float32
-// instruction.
+// bfloat16: what is computed on the way (scores, states, faded values) enters a product as a sum of three bfloat16, 24 bits: exactly.
+// float32: the float32 instruction.
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -205,7 +204,11 @@ struct alignas(16) ChunkLds {
     // their rows too, see swizzle().
     static constexpr int K = 32 * KT, V = 32 * NC, PAD = 16 / (int)sizeof(T), ACROSS = DT == kBF16 ? 0 : PAD;
     T k[kChunk][K + ACROSS], v[kChunk][V + ACROSS], q[OUT ? kChunk : 1][K + PAD];
-    T p[DT == kBF16 ? 2 : 1][OUT ? kChunk : 1][kChunk + PAD]; // scores, by query; bfloat16: in two parts
+    // Scores, by query; bfloat16: in three parts, and the first 32 queries have rows of 32 keys, so that two workgroups of two tiles and keys
+    // of 128 find room in a compute unit.
+    static constexpr int LONG = kChunk + PAD, SHORT = DT == kBF16 ? kChunk / 2 + PAD : LONG, PARTS = DT == kBF16 ? 3 : 1;
+    static __device__ __forceinline__ int query(int i) { return SHORT == LONG || i < kChunk / 2 ? i * SHORT : kChunk / 2 * SHORT + (i - kChunk / 2) * LONG; }
+    T p[PARTS][OUT ? kChunk / 2 * (SHORT + LONG) : 1];
     f32x4 other[OUT ? 2 * NC : 1][4][64]; // a wave's part of Q S for the queries of the wave beside it
     float fade_v[kChunk];        // g^(m-1) ... g^0 of the chunk at hand, then ones
     float fade_q[kChunk];        // scale g^1 ... scale g^64
@@ -321,8 +324,8 @@ __global__ __launch_bounds__(NC * 128, NC == 4 || DT == kBF16 ? 2 : 1) void chun
     if (OUT) // scores of later keys in the tiles that are multiplied all the same
         for (int i = threadIdx.x; i < 2 * 16 * 16; i += NT) {
             const int at = i >> 8, row = 32 * at + (i >> 4 & 15), col = 32 * at + 16 + (i & 15);
-            lds.p[0][row][col] = 0;
-            lds.p[DT == kBF16][row][col] = 0;
+#pragma unroll
+            for (int part = 0; part < Lds::PARTS; ++part) lds.p[part][Lds::query(row) + col] = 0;
         }
 
     // rows of S: row0 + 32 kt + 8 (r / 4) + r % 4 for register r; the lane's column
@@ -450,11 +453,16 @@ __global__ __launch_bounds__(NC * 128, NC == 4 || DT == kBF16 ? 2 : 1) void chun
                 float x[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[e] = i >= j + e ? p[e] * fade[e] : 0.0f;
+                const int to = Lds::query(i) + j;
                 if constexpr (DT == kBF16) {
-                    *reinterpret_cast<uint2 *>(&lds.p[0][i][j]) = make_uint2(upper_halves(x[0], x[1]), upper_halves(x[2], x[3]));
-                    *reinterpret_cast<uint2 *>(&lds.p[DT == kBF16][i][j]) = make_uint2(bf16_pair(x[0] - cut(x[0]), x[1] - cut(x[1])), bf16_pair(x[2] - cut(x[2]), x[3] - cut(x[3])));
+#pragma unroll
+                    for (int part = 0; part < Lds::PARTS; ++part) {
+                        *reinterpret_cast<uint2 *>(&lds.p[part][to]) = make_uint2(upper_halves(x[0], x[1]), upper_halves(x[2], x[3]));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] -= cut(x[e]);
+                    }
                 } else {
-                    *reinterpret_cast<f32x4 *>(&lds.p[0][i][j]) = f32x4{x[0], x[1], x[2], x[3]};
+                    *reinterpret_cast<f32x4 *>(&lds.p[0][to]) = f32x4{x[0], x[1], x[2], x[3]};
                 }
             }
             // this wave's rows of S in Q S
@@ -466,16 +474,17 @@ __global__ __launch_bounds__(NC * 128, NC == 4 || DT == kBF16 ? 2 : 1) void chun
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
                         float x[8];
-                        u32x4 y[2];
+                        u32x4 y[3];
 #pragma unroll
                         for (int e = 0; e < 8; ++e) x[e] = S[kt][8 * s + e];
                         split(x, y);
                         const T *qp = &lds.q[32 * low + side][32 * (KH * low + kt) + 16 * s + 8 * half];
                         const u32x4 z0 = *reinterpret_cast<const u32x4 *>(qp), z1 = *reinterpret_cast<const u32x4 *>(qp + across);
-                        qs[0] = multiply(z0, y[0], qs[0]);
-                        qs[1] = multiply(z1, y[0], qs[1]);
-                        qs[0] = multiply(z0, y[1], qs[0]);
-                        qs[1] = multiply(z1, y[1], qs[1]);
+#pragma unroll
+                        for (int i = 0; i < 3; ++i) {
+                            qs[0] = multiply(z0, y[i], qs[0]);
+                            qs[1] = multiply(z1, y[i], qs[1]);
+                        }
                     }
                 } else {
 #pragma unroll
@@ -542,18 +551,19 @@ __global__ __launch_bounds__(NC * 128, NC == 4 || DT == kBF16 ? 2 : 1) void chun
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[4 * c + e] = (acc[4 * c + e] + x[e]) * f[e];
             }
+            const T *scores = &lds.p[0][Lds::query(32 * low + side)];
             if (!lds.odd[turn]) {
                 if constexpr (DT == kBF16) {
 #pragma unroll
                     for (int s = 0; s < 4; ++s)
                         if (s < 2 + 2 * low)
 #pragma unroll
-                            for (int i = 0; i < 2; ++i) acc = multiply(*reinterpret_cast<const u32x4 *>(&lds.p[DT == kBF16 ? i : 0][32 * low + side][16 * s + 8 * half]), vs[s], acc);
+                            for (int i = 0; i < 3; ++i) acc = multiply(*reinterpret_cast<const u32x4 *>(scores + i * (sizeof(lds.p[0]) / sizeof(T)) + 16 * s + 8 * half), vs[s], acc);
                 } else {
 #pragma unroll
                     for (int c = 0; c < 8; ++c)
                         if (c < 4 + 4 * low) {
-                            const f32x4 z = *reinterpret_cast<const f32x4 *>(&lds.p[0][32 * low + side][8 * c + 4 * half]);
+                            const f32x4 z = *reinterpret_cast<const f32x4 *>(scores + 8 * c + 4 * half);
 #pragma unroll
                             for (int e = 0; e < 4; ++e) acc = multiply(z[e], __uint_as_float(vs[c % (DT == kBF16 ? 4 : 8)][e]), acc);
                         }
@@ -565,8 +575,9 @@ __global__ __launch_bounds__(NC * 128, NC == 4 || DT == kBF16 ? 2 : 1) void chun
                     for (int r = 0; r < 16; ++r) {
                         const int i = i0 + 8 * (r / 4) + r % 4;
                         if (i >= j) {
-                            float p = Elem<DT>::get(lds.p[0][i][j]);
-                            if (DT == kBF16) p += Elem<DT>::get(lds.p[DT == kBF16][i][j]);
+                            float p = 0.0f;
+#pragma unroll
+                            for (int part = Lds::PARTS - 1; part >= 0; --part) p += Elem<DT>::get(lds.p[part][Lds::query(i) + j]);
                             acc[r] = __builtin_fmaf(p, x, acc[r]);
                         }
                     }
@@ -636,24 +647,24 @@ struct Plan {
 Plan plan(const cbinfer_linear_attention_args &a)
 {
     Plan p = {false, 1, 1, 1, 4};
-    // us for 64 streams, 16 heads of 128 x 128, token after token and in chunks: bfloat16 4 tokens 36, 37, 6 tokens 44, 36, 15 tokens 77, 37; float32 12
-    // tokens 57, 75; 16 streams, 8 heads, float32 15 tokens: 19, 17.
+    // us for 64 streams, 16 heads of 128 x 128, token after token and in chunks: bfloat16 4 tokens 36.5, 40.2, 5 tokens 40.1, 39.5, 8 tokens 51, 39; float32
+    // 12 tokens 57, 75; 16 streams, 8 heads, bfloat16 4 tokens 8.7, 9.4, 5 tokens 9.7, 9.4, float32 15 tokens: 19, 17.
     if (a.tokens < (a.dtype == kF32 ? 16 : 5)) return p;
     p.chunks = true;
     const int tiles = (a.value_size + 31) / 32;
     const int64_t heads = (int64_t)a.streams * a.heads, chunks = (a.tokens + kChunk - 1) / kChunk;
     // Two tiles where all chunks together do not fill the chip twice: their scores are computed twice, but four waves are through sooner
-    // than eight.  us for 82 tokens, 4 heads of 96 x 128 float32: 24, four tiles 28; 8192 tokens, 16 heads: 99, 72.
+    // than eight.  us for 82 tokens, 4 heads of 96 x 128 float32: 24, four tiles 28; 8192 tokens, 16 heads: 86, 77.
     p.tiles = (a.dtype == kF32 || a.key_size <= 128) && (tiles <= 2 || heads * ((tiles + 1) / 2) * chunks <= 512) ? 2 : 4;
     p.slices = (tiles + p.tiles - 1) / p.tiles;
     const int64_t groups = heads * p.slices;
-    // Parts until every compute unit has a workgroup; their keys and values are read twice.  us for 8192 tokens, 16 heads of 128: 8 parts 119,
-    // 16 72, 20 96.  Streams of different lengths leave compute units idle: half as many again (12 streams of up to 1023 tokens, 6 heads,
+    // Parts until every compute unit has a workgroup; their keys and values are read twice.  us for 8192 tokens, 16 heads of 128: 8 parts 107,
+    // 16 78, 20 107.  Streams of different lengths leave compute units idle: half as many again (12 streams of up to 1023 tokens, 6 heads,
     // float32: 3 parts 83, 6 62, 7 70, 8 64).  Of two tiles in bfloat16 a compute unit takes two workgroups (6 streams of 1749 tokens, 12 heads
-    // of 96 x 64: 52, with one 67).
+    // of 96 x 64: 51, with one 64).
     const int64_t room = (a.lengths ? 400 : 256) * (p.tiles == 2 && a.dtype == kBF16 ? 2 : 1);
-    // From 256 on they do not pay (16 streams of up to 500 tokens, 16 heads of 64 x 64: 28, in three parts 33); below, already with three chunks
-    // (2 streams of 190 tokens, 16 heads of 128 x 128: 15.1, in three parts 13.7; two chunks, 2 streams of 100, 4 heads of 64 x 64: 9.2, 11.6), in
+    // From 256 on they do not pay (16 streams of up to 500 tokens, 16 heads of 64 x 64: 32, in three parts 35); below, already with three chunks
+    // (2 streams of 190 tokens, 16 heads of 128 x 128: 16.6, in three parts 14.1; two chunks, 2 streams of 100, 4 heads of 64 x 64: 10.3, 11.9), in
     // float32 with two (4 streams of 100 tokens, 4 heads of 64 x 128: 18.6, 17.0).
     const bool pays = groups < 256 && chunks > (a.dtype == kF32 ? 1 : 2);
     p.parts = pays ? (int)std::max<int64_t>(1, std::min(chunks, room / std::max<int64_t>(groups, 1))) : 1;
@@ -680,7 +691,7 @@ hipError_t chunked(hipStream_t st, const cbinfer_linear_attention_args &a, const
 }
 
 constexpr int kKeys = 128; // at a time, float32
-constexpr int kFold = 16; // parts up to which the outputs' kernel joins them: 4 streams of 1000 tokens, 16 heads of 128 x 128, 4 parts: 39 us, joined before 49; one of 8192, 16 parts: 72, 76
+constexpr int kFold = 16; // parts up to which the outputs' kernel joins them: 4 streams of 1000 tokens, 16 heads of 128 x 128, 4 parts: 43 us, joined before 51; one of 8192, 16 parts: 75, 74
 
 template <int DT, bool WHOLE>
 hipError_t chunked_any(hipStream_t st, const cbinfer_linear_attention_args &a, const Plan &p)

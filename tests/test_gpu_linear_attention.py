@@ -157,3 +157,35 @@ def test_more_parts_than_an_output_joins(dtype):
     _run(1, 1500, 1, 1, 64, 48, dtype, what="many parts")
     _run(2, 1300, 1, 1, 160, 32, dtype, lengths=[1300, 700], what="many parts, ragged")
     _run(3, 1100, 1, 1, 32, 32, dtype, lengths=[64, 65, 1088], what="a chunk, and one token more")
+
+
+def _integers(T, d, seed, wide):
+    """Whole numbers whose sums of products stay below 2^24, so that they are exact in float32 in any order, although they cancel: what is
+    added up has far more bits than the result.  `wide` "scores": queries and keys of 8 bits, keys of neighbours opposite but for one
+    place, values +-1.  "state": entries of 18 bits, neighbours opposite but for their last bits."""
+    g = torch.Generator().manual_seed(seed)
+    whole = lambda m, *s: torch.randint(-m, m + 1, s, generator=g).float()  # noqa: E731
+    state = torch.zeros(1, 1, d, d)
+    if wide == "scores":
+        q, k, v = whole(255, 1, T, 1, d), whole(127, 1, T, 1, d), 2 * torch.randint(0, 2, (1, T, 1, d), generator=g).float() - 1
+        k[:, 1::2] = -k[:, :T // 2 * 2:2]
+        k[:, 1::2, :, 3] += 1
+        v[:, 1::2] = v[:, :T // 2 * 2:2]
+    else:
+        q, k, v = whole(1, 1, T, 1, d), torch.zeros(1, T, 1, d), torch.zeros(1, T, 1, d)
+        q[..., 1::2] = q[..., ::2]
+        state[:, :, ::2] = whole(2 ** 18 - 8, 1, 1, d // 2, d)
+        state[:, :, 1::2] = whole(3, 1, 1, d // 2, d) - state[:, :, ::2]
+    return q, k, v, state
+
+
+@pytest.mark.parametrize("wide", ["scores", "state"])
+@pytest.mark.parametrize("T,d", [(1, 64), (5, 64), (15, 128), (64, 32), (150, 64), (150, 128), (90, 256)])
+def test_scores_and_states_keep_24_bits(T, d, wide):
+    q, k, v, state = _integers(T, d, T + d, wide)
+    att = cb.LinearAttention([1.0], d, d)
+    att.state.copy_(state)
+    want, S, _, _ = attention64(q, k, v, state, [1.0], 1.0, None)
+    out = att.process(*(t.bfloat16().cuda() for t in (q, k, v)))
+    assert torch.equal(att.state.cpu().double(), S)
+    assert torch.equal(out.cpu(), want.to(torch.bfloat16))
