@@ -23,9 +23,26 @@ __device__ __forceinline__ float block_sum(float v, float *scratch)
     return (scratch[0] + scratch[1]) + (scratch[2] + scratch[3]);
 }
 
+// exp(-|g|), which never overflows, so that gates far below zero keep their bits down to the smallest number.  As the square of
+// 2^(-|g| log2(e) / 2), which is a normal number wherever the square is any; log2(e) / 2 in two parts, the first of which times a bfloat16
+// is exact, and what its product with a float32 is rounded by, make up for an exponent that would be off by up to 2^-18.
+template <int DT>
+__device__ __forceinline__ float exp_down(float g)
+{
+    constexpr double kHalf = 0.72134752044448170368, kLn4 = 1.38629436111989061883;
+    constexpr float kFirst = DT == kBF16 ? 47274.0f / 65536.0f : (float)kHalf, kRest = (float)((kHalf - kFirst) * kLn4);
+    static_assert(DT != kBF16 || kRest > 0.0f, "a factor below 1");
+    const float a = -fabsf(g), t = a * kFirst, e = __builtin_amdgcn_exp2f(t);
+    float f = __builtin_fmaf(a, kRest, 1.0f);
+    if (DT == kF32) f = __builtin_fmaf(__builtin_fmaf(a, kFirst, -t), (float)kLn4, f);
+    f = DT == kF32 ? __builtin_amdgcn_fmed3f(f, 0.5f, 2.0f) : __builtin_amdgcn_fmed3f(f, 0.0f, 1.0f); // infinite or NaN where g is infinite, and e is 0
+    return e * e * f;
+}
+
+template <int DT>
 __device__ __forceinline__ float gate_of(float g, int kind)
 {
-    const float open = __builtin_amdgcn_rcpf(1.0f + __expf(-g));
+    const float e = exp_down<DT>(g), most = __builtin_amdgcn_rcpf(1.0f + e), open = g < 0.0f ? e * most : most;
     return kind == CBINFER_GATE_SIGMOID ? open : g * open;
 }
 
@@ -60,7 +77,7 @@ __global__ __launch_bounds__(256) void norm_row_kernel(const cbinfer_gated_norm_
     for (int i = threadIdx.x; i < d; i += 256) {
         float u = row[i];
         if (a.weight) u *= factor[i / group] * a.weight[i];
-        if (a.gate) u *= gate_of(Elem<DT>::get(gate[i]), a.gate_kind);
+        if (a.gate) u *= gate_of<DT>(Elem<DT>::get(gate[i]), a.gate_kind);
         u *= a.scale;
         if (a.channel_scale) u *= a.channel_scale[i];
         if (a.residual) u += Elem<DS>::get(residual[i]);
@@ -223,7 +240,7 @@ __global__ __launch_bounds__(MOST < 256 ? 256 : MOST) void norm_kernel(const cbi
             if (there[i]) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    if (a.gate) u[i][e] *= gate_of(gs[i].get(e), a.gate_kind);
+                    if (a.gate) u[i][e] *= gate_of<DT>(gs[i].get(e), a.gate_kind);
                     u[i][e] = a.residual ? __builtin_fmaf(u[i][e], scale[i][e], rs[i].get(e)) : u[i][e] * scale[i][e];
                     sum = __builtin_fmaf(u[i][e], u[i][e], sum);
                 }

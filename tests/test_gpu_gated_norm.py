@@ -138,3 +138,46 @@ def test_no_rows(kind, sum_kind):
     x, w = torch.empty(0, 24, dtype=kind, device="cuda"), torch.ones(24, device="cuda")
     h, y = cb.gated_norm(x, w, group=8, residual=torch.empty(0, 24, dtype=sum_kind, device="cuda"), next_weight=w)
     assert h.shape == y.shape == (0, 24) and h.dtype == sum_kind and y.dtype == kind
+
+
+@pytest.mark.parametrize("activation", ["silu", "sigmoid"])
+@pytest.mark.parametrize("d", [1000, 1023, 99])
+def test_gates_of_any_size(d, activation):
+    """The bound of _check holds for every gate: the exponential of a large argument is as exact as that of a small one."""
+    t = _all(4, d, torch.float32, torch.float32)
+    gate = torch.linspace(-87.0, 87.0, 4 * d).view(4, d).cuda()
+    for group in (0, 11) if d == 99 else (0,):
+        kw = dict(weight=t["weight"], group=group, gate=gate, activation=activation)
+        h, _ = cb.gated_norm(t["x"], **kw)
+        want, _, most, _ = norm64(t["x"], residual=None, scale=1.0, next_weight=None, eps=EPS, **kw)
+        # some are below the normal numbers: h is the rounding to float32 of a value within the bound
+        low, high = (want - 2.0 ** -20 * most).float(), (want + 2.0 ** -20 * most).float()
+        assert bool(((h.cpu() >= low) & (h.cpu() <= high)).all())
+
+
+@pytest.mark.parametrize("activation", ["silu", "sigmoid"])
+def test_gates_whose_exponential_is_no_normal_number(activation):
+    """From -87.4 on e^g is below the normal numbers: results are off by a step of what float32 has there (2^-149) for each of three
+    roundings, times the gate where it multiplies."""
+    gate = torch.linspace(-110.0, -87.4, 128).view(2, 64).cuda()
+    h, _ = cb.gated_norm(torch.ones(2, 64, device="cuda"), gate=gate, activation=activation)
+    g = gate.cpu().double()
+    want = 1 / (1 + (-g).exp()) * (g if activation == "silu" else 1.0)
+    off = (h.cpu().double() - want).abs()
+    assert bool((off <= 2.0 ** -20 * want.abs() + 3 * 2.0 ** -149 * (g.abs() if activation == "silu" else 1.0)).all()), float(off.max())
+
+
+@pytest.mark.parametrize("activation", ["silu", "sigmoid"])
+def test_bfloat16_gates_of_any_size(activation):
+    """The same bound with gates of 8 bits and a result of 24."""
+    d = 1024
+    t = _all(4, d, torch.bfloat16, torch.float32)
+    gate = torch.linspace(-86.0, 86.0, 4 * d).view(4, d).to(torch.bfloat16).cuda()
+    x, zero = torch.ones(4, d, dtype=torch.bfloat16, device="cuda"), torch.zeros(4, d, device="cuda")
+    kw = dict(weight=t["weight"], gate=gate, activation=activation, residual=zero)
+    _check(*cb.gated_norm(x, **kw), x, "gates", **kw)
+    for bad, want in ((float("inf"), float("inf") if activation == "silu" else 1.0), (float("nan"), float("nan")),
+                      (float("-inf"), float("nan") if activation == "silu" else 0.0)):
+        for kind in (torch.bfloat16, torch.float32):
+            h, _ = cb.gated_norm(x.to(kind), gate=torch.full_like(x, bad, dtype=kind), activation=activation)
+            assert bool((h.float() == want).all() if want == want else h.isnan().all()), (bad, kind)
