@@ -129,7 +129,8 @@ struct Eight {
     __device__ __forceinline__ float get(int e) const { return Unit<DT>::get(u[DT == kF32 ? e / 4 : 0], DT == kF32 ? e % 4 : e); }
 };
 
-// A float as the sum of three bfloat16, exactly: eight bits are cut off each time.  Infinities stay in the first.
+// A float as the sum of three bfloat16, exactly: eight bits are cut off each time.  Infinities stay in the first; a NaN, of
+// which that may leave an infinity, is in the others.
 __device__ __forceinline__ void parts_of(const Eight<kBF16> &v, bf16x8 (&p)[1]) { p[0] = __builtin_bit_cast(bf16x8, v.u[0]); }
 __device__ __forceinline__ void parts_of(const Eight<kF32> &v, bf16x8 (&p)[3])
 {
@@ -147,7 +148,7 @@ __device__ __forceinline__ void parts_of(const Eight<kF32> &v, bf16x8 (&p)[3])
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float top = __uint_as_float(__float_as_uint(r[e]) & 0xffff0000u);
-                r[e] = __builtin_isinf(top) ? 0.0f : r[e] - top;
+                r[e] = __builtin_isinf(r[e]) ? 0.0f : r[e] - top;
             }
     }
 }

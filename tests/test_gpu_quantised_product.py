@@ -206,3 +206,14 @@ def test_a_layer_used_by_two_threads():
         t.join()
     for i in (0, 1):
         assert len(got[i]) == 200 and all(torch.equal(y, alone[i]) for y in got[i])
+
+
+def test_every_nan_stays_a_nan():
+    """float32 NaN whatever its bits: those that are told from infinity by their last bits too."""
+    layer = _layer(32, 200, 64, 5, bias=False)[3]
+    bits = torch.tensor([0x7f800001, 0x7f80ffff, 0x7fc00000, 0x7fffffff, 0x7f810000], dtype=torch.int64)
+    bits = torch.cat([bits, bits | 0x80000000])
+    x = torch.randn(20, 200, generator=torch.Generator().manual_seed(2))
+    x.view(torch.int32)[torch.arange(10), 13 * torch.arange(10)] = bits.to(torch.int32)
+    got = layer(x.cuda()).cpu()
+    assert bool(got[:10].isnan().all()) and bool(got[10:].isfinite().all())
