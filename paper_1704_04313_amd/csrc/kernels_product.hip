@@ -233,7 +233,8 @@ __global__ __launch_bounds__(WAVES * 64, WAVES * PER_CU / 4) void product_kernel
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const uint4 w = k.w[r][i];
-                const uint2 s2 = k.s[r][i];
+                // beyond the last block: infinite scales would make NaN of the zeros
+                const uint2 s2 = block0 + i * WAVES < blocks ? k.s[r][i] : make_uint2(0, 0);
                 f32x4 part[MT];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {

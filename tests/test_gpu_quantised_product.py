@@ -217,3 +217,19 @@ def test_every_nan_stays_a_nan():
     x.view(torch.int32)[torch.arange(10), 13 * torch.arange(10)] = bits.to(torch.int32)
     got = layer(x.cuda()).cpu()
     assert bool(got[:10].isnan().all()) and bool(got[10:].isfinite().all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m", [1, 16, 33, 64])
+@pytest.mark.parametrize("n,k", [(40, 1200), (40, 600), (16400, 1200), (600, 4500)])
+def test_infinite_scales(m, n, k, dtype):
+    """A scale that is infinite makes its row's results infinite: no column that is not there turns them into NaN."""
+    g = torch.Generator().manual_seed(m + n)
+    codes = torch.randint(1, 8, (n, k), generator=g, dtype=torch.uint8)
+    scales = (0.02 + torch.rand(n, -(-k // 64), generator=g)).to(torch.bfloat16)
+    scales[3, -1], scales[5, 0] = float("inf"), float("inf")
+    x = (0.1 + torch.rand(m, k, generator=g)).to(dtype)
+    got = cb.QuantisedLinear(codes.cuda(), scales.cuda(), group=64)(x.cuda()).cpu()
+    want = torch.zeros(n, dtype=torch.bool)
+    want[3] = want[5] = True
+    assert bool((got[:, want] == float("inf")).all()) and bool(got[:, ~want].isfinite().all())
