@@ -76,9 +76,9 @@ __global__ __launch_bounds__(256) void pack_scales_kernel(const uint16_t *scales
 
 // 32 lanes a group; 100003 x 2048 float32 436 us.
 template <int DT>
-__global__ __launch_bounds__(256) void quantise_kernel(const typename Elem<DT>::type *w, int64_t rows, int64_t cols, int64_t stride, int group, int64_t groups, uint8_t *codes, uint16_t *scales)
+__global__ __launch_bounds__(256) void quantise_kernel(const typename Elem<DT>::type *w, int64_t rows, int64_t cols, int64_t stride, int group, int64_t groups, int64_t first, uint8_t *codes, uint16_t *scales)
 {
-    const int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int64_t at = first + (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     if (at >= rows * groups) return;
     const int64_t n = at / groups, k0 = (at - n * groups) * group;
     const int lane = threadIdx.x & 31;
@@ -398,12 +398,16 @@ hipError_t quantise_weights(hipStream_t st, const void *weights, int dtype, int6
                             int group, uint8_t *codes, uint16_t *scales)
 {
     const int64_t groups = (cols + group - 1) / group;
-    const unsigned grid = (unsigned)((rows * groups + 7) / 8);
-    if (dtype == kF32)
-        quantise_kernel<kF32><<<grid, 256, 0, st>>>(static_cast<const float *>(weights), rows, cols, row_stride, group, groups, codes, scales);
-    else
-        quantise_kernel<kBF16><<<grid, 256, 0, st>>>(static_cast<const uint16_t *>(weights), rows, cols, row_stride, group, groups, codes, scales);
-    return hipGetLastError();
+    constexpr int64_t kMostBlocks = 1 << 22; // of a launch: threads are counted in 32 bits
+    for (int64_t first = 0; first < rows * groups; first += 8 * kMostBlocks) {
+        const unsigned grid = (unsigned)std::min(kMostBlocks, (rows * groups - first + 7) / 8);
+        if (dtype == kF32)
+            quantise_kernel<kF32><<<grid, 256, 0, st>>>(static_cast<const float *>(weights), rows, cols, row_stride, group, groups, first, codes, scales);
+        else
+            quantise_kernel<kBF16><<<grid, 256, 0, st>>>(static_cast<const uint16_t *>(weights), rows, cols, row_stride, group, groups, first, codes, scales);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
 }
 
 size_t packed_weights_bytes(int64_t rows, int64_t cols, int group)

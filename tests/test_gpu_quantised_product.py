@@ -233,3 +233,17 @@ def test_infinite_scales(m, n, k, dtype):
     want = torch.zeros(n, dtype=torch.bool)
     want[3] = want[5] = True
     assert bool((got[:, want] == float("inf")).all()) and bool(got[:, ~want].isfinite().all())
+
+
+@pytest.mark.parametrize("rows,cols", [(1 << 16, 1 << 16), (66000000, 65)])
+def test_quantising_as_many_weights_as_there_may_be(rows, cols):
+    """Groups of 32 that need more threads than a launch has: the first rows, the last, some in the middle."""
+    few = torch.randn(512, cols, generator=torch.Generator().manual_seed(3)).to(torch.bfloat16).cuda()
+    places = [0, rows // 3, 2 * rows // 3, rows - 512]
+    w = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    for at in places:
+        w[at:at + 512] = few
+    want = cb.quantise_weights(few, 32)
+    codes, scales = cb.quantise_weights(w, 32)
+    for at in places:
+        assert torch.equal(codes[at:at + 512], want[0]) and torch.equal(scales[at:at + 512], want[1]), at
