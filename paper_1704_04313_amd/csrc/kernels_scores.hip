@@ -181,10 +181,10 @@ __device__ void careful_top(const cbinfer_log_probs_args &a, int64_t base, int64
     int key = kNone, index = -1; // the one found last; first: as if in front of every other
     for (int j = 0; j < a.top; ++j) {
         int bk = -kNone - 1, bi = kNone;
-        for (int c = lane; c < (int)a.classes; c += 64) {
+        for (int64_t c = lane; c < a.classes; c += 64) { // 64 beyond the last may pass 31 bits
             const int k = rank_key(score<DT>(a, base + c * a.class_stride));
             const bool behind = j == 0 || k < key || (k == key && c > index);
-            if (behind && (k > bk || (k == bk && c < bi))) { bk = k; bi = c; }
+            if (behind && (k > bk || (k == bk && c < bi))) { bk = k; bi = (int)c; }
         }
         for (int off = 32; off; off >>= 1) {
             const int ok = __shfl_xor(bk, off), oi = __shfl_xor(bi, off);
@@ -325,7 +325,7 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64, DT == kBF16 ? 8 : 1) 
     b.begin(buffers[threadIdx.x >> 6], k);
     auto few = [&](int from, int to) { // fewer than 64, by the first wave
         if (from >= to || wave != 0) return;
-        const bool there = from + lane < to;
+        const bool there = lane < to - from; // their sum may pass 31 bits
         const float v = there ? Elem<DT>::get(x[from + lane]) : -__builtin_inff();
         if (v > t.m) raise_to(t, v);
         add(t, v);
@@ -762,9 +762,9 @@ Plan plan(const cbinfer_log_probs_args &a)
         // 64 rows of 100003 bfloat16: 29 us whole, 18 in segments, join included; one of 131071: 28 and 14.
         const int64_t round = 4 * 64 * 4 * (a.dtype == kF32 ? 4 : 8), segments = std::min<int64_t>({(a.classes + round - 1) / round, 64, 1024 / std::max<int64_t>(positions, 1)});
         if (segments >= 4) p.segments = (int)segments;
-    } else if (a.inner_stride == 1 && a.inner >= 16 && (a.outer == 1 || a.outer_stride >= a.inner) && a.top <= 16 && (a.classes <= 1024 || positions >= 16384) &&
+    } else if (a.classes <= 1 << 30 && a.inner_stride == 1 && a.inner >= 16 && (a.outer == 1 || a.outer_stride >= a.inner) && a.top <= 16 && (a.classes <= 1024 || positions >= 16384) &&
                (a.dtype == kF32 || a.classes <= Key<kBF16>::kClasses)) {
-        p.kind = kMaps;
+        p.kind = kMaps; // counts classes in whole rounds and parts, in 32 bits
         // 5 x 191 x 148 x 269 bfloat16, 3 alternatives: a wave each 35 us, four waves 29; float32 without: 28, 33
         p.waves = positions < (a.top ? 262144 : 65536) && a.classes >= 32 ? 4 : 1;
     }

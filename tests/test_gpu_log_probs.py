@@ -200,3 +200,20 @@ def test_maps_with_fewer_live_classes_than_alternatives(classes, top, dtype):
     x = x.to(dtype).cuda()
     labels = _labels((2, 6, 16), classes, top)
     check_log_probs(cb.log_probs(x, labels, top=top), x, labels, 1, top, "%d classes, %d best" % (classes, top))
+
+
+@pytest.mark.parametrize("dtype,classes", [(torch.bfloat16, 2 ** 31 - 1), (torch.float32, 2 ** 31 - 1), (torch.bfloat16, 2 ** 31 - 64)])
+def test_as_many_classes_as_there_may_be(dtype, classes):
+    """One row of 2^31 - 1 scores: the last ones are the best, in front of the last whole 16 bytes and behind."""
+    x = torch.full((1, classes), -30.0, dtype=dtype, device="cuda")
+    best = {classes - 1: 2.0, 0: 1.0, classes - 9: 3.0, 2 ** 30 + 1: 0.5, classes - 2: 0.0}
+    for at, value in best.items():
+        x[0, at] = value
+    got = cb.log_probs(x, torch.tensor([classes - 1], device="cuda"), top=5)
+    order = sorted(best, key=lambda c: -best[c])
+    every = torch.tensor([best[c] for c in order], dtype=torch.float64)
+    # 2^31 terms of e^-30 are 2e-4: of their sum's roundings (4 sqrt(2^31) at most) nothing reaches the logarithm's last bits
+    log_s = (every.exp().sum() + (classes - 5) * torch.tensor(-30.0, dtype=torch.float64).exp()).log()
+    assert got.index[0].tolist() == order
+    torch.testing.assert_close(got.top[0].cpu().double(), every - log_s, rtol=0, atol=1e-5)
+    torch.testing.assert_close(got.label[0].cpu().double(), 2.0 - log_s, rtol=0, atol=1e-5)
