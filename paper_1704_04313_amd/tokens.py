@@ -278,6 +278,8 @@ class LinearAttention:
             _refuse("key and value sizes must be 1 .. 256 (got %d and %d)" % (key_size, value_size))
         if n_streams < 1:
             _refuse("n_streams must be >= 1")
+        if n_streams * self.heads > 1 << 18:  # here, as the library is told of 32 bits
+            _refuse("streams times heads must be at most 2^18 (got %d and %d)" % (n_streams, self.heads))
         self.n_streams, self.key_size, self.value_size, self.scale = int(n_streams), int(key_size), int(value_size), float(scale)
         self.decay = torch.tensor(decay, dtype=torch.float32).cuda()
         self._state = torch.zeros((self.n_streams, self.heads, self.key_size, self.value_size), dtype=torch.float32,
@@ -334,6 +336,8 @@ class LinearAttention:
         if q.dim() != 4:
             _refuse("q must be [streams][tokens][heads][key_size]")
         tokens = q.shape[1]
+        if tokens > 1 << 28:
+            _refuse("tokens must be at most 2^28 (got %d)" % tokens)
         for t, n, size, what in ((q, self.heads, self.key_size, "q"), (k, self.kv_heads, self.key_size, "k"),
                                  (v, self.kv_heads, self.value_size, "v")):
             if t.shape != (self.n_streams, tokens, n, size):
@@ -382,6 +386,8 @@ class QuantisedLinear:
             _refuse("codes must be a contiguous uint8 matrix")
         device = _device(codes, "codes")
         self.rows, self.cols = codes.shape
+        if group not in (32, 64, 128):
+            _refuse("a group must be 32, 64 or 128 weights (got %r)" % (group,))
         self.group = int(group)
         nbytes = self.lib.cbinfer_packed_weights_bytes(self.rows, self.cols, self.group)
         if not nbytes:
@@ -527,6 +533,8 @@ def _norm_plan(x, weight, group, gate, activation, residual, next_weight, eps, s
     a.eps = eps
     a.rows, a.x_stride = _norm_rows(x, shape, "x")
     if weight is not None:
+        if not 0 <= group <= a.size:
+            _refuse("group must be 0 or divide the size, %d (got %r)" % (a.size, group))
         a.group = group
     elif group:
         _refuse("group without weight")

@@ -248,3 +248,20 @@ def test_attention_called_by_two_threads(recorder, first):
             assert (a.tokens, a.o) == (q.shape[1], out.data_ptr()) and out.shape == (1, q.shape[1], 2, 32)
             assert list(a.q_stride) == list(q.stride()[:3]) and list(a.o_stride) == list(out.stride()[:3])
             assert a.workspace_bytes >= recorder.lib.cbinfer_linear_attention_workspace_bytes(a)
+
+
+def test_sizes_beyond_32_bits_are_refused(recorder, monkeypatch):
+    """What the library takes as 32 bits is checked before it is cut to them: 2^32 + 32 is not 32."""
+    launches = []
+    monkeypatch.setattr(tokens, "_lib", type("Lib", (), {"cbinfer_gated_norm": lambda self, a, stream: launches.append(a) or 0})())
+    x, one = torch.zeros(2, 12), torch.zeros(1)
+    att = cb.LinearAttention([0.9], 1, 1)
+    for call, message in (
+            (lambda: cb.QuantisedLinear(torch.zeros(4, 96, dtype=torch.uint8), torch.zeros(4, 1, dtype=torch.bfloat16), group=2 ** 32 + 32), "group"),
+            (lambda: cb.gated_norm(x, torch.ones(12), group=2 ** 32 + 3), "group"),
+            (lambda: cb.gated_norm(x, torch.ones(12), group=2 ** 32), "group"),
+            (lambda: att.process(*(one.expand(1, 2 ** 32 + 3, 1, 1) for _ in range(3))), "tokens"),
+            (lambda: cb.LinearAttention([0.9], 1, 1, n_streams=2 ** 32 + 1), "streams")):
+        with pytest.raises(cb.CBInferError, match=message):
+            call()
+    assert not launches and not recorder.calls
