@@ -281,19 +281,24 @@ class LinearAttention:
         if n_streams * self.heads > 1 << 18:  # here, as the library is told of 32 bits
             _refuse("streams times heads must be at most 2^18 (got %d and %d)" % (n_streams, self.heads))
         self.n_streams, self.key_size, self.value_size, self.scale = int(n_streams), int(key_size), int(value_size), float(scale)
-        self.decay = torch.tensor(decay, dtype=torch.float32).cuda()
+        self._decay = torch.tensor(decay, dtype=torch.float32).cuda()
         self._state = torch.zeros((self.n_streams, self.heads, self.key_size, self.value_size), dtype=torch.float32,
-                                  device=self.decay.device)
+                                  device=self._decay.device)
         self._plan: Optional[_LayerPlan] = None
         a = self._args = linear_attention_args()
         a.streams, a.heads, a.kv_heads = self.n_streams, self.heads, self.kv_heads
         a.key_size, a.value_size, a.scale = self.key_size, self.value_size, self.scale
-        a.state, a.decay = self._state.data_ptr(), self.decay.data_ptr()
+        a.state, a.decay = self._state.data_ptr(), self._decay.data_ptr()
 
     @property
     def state(self):
         """[n_streams][heads][key_size][value_size] float32; filled in place to restore what was saved."""
         return self._state
+
+    @property
+    def decay(self):
+        """[heads] float32."""
+        return self._decay
 
     def reset(self):
         """Forget what the streams have seen."""
@@ -398,7 +403,7 @@ class QuantisedLinear:
         _same_device(scales, device, "scales")
         if bias is not None:
             _float32(bias, device, self.rows, "bias")
-        self.bias = bias
+        self._bias = bias
         self._memory = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
         packed = (self._memory.data_ptr() + 255) // 256 * 256
         rc = self.lib.cbinfer_pack_weights(codes.data_ptr(), scales.data_ptr(), self.rows, self.cols, self.group, packed, _stream(device))
@@ -408,6 +413,11 @@ class QuantisedLinear:
         a = self._args = quantised_product_args()
         a.group, a.rows, a.cols, a.packed = self.group, self.rows, self.cols, packed
         a.bias = None if bias is None else bias.data_ptr()
+
+    @property
+    def bias(self):
+        """[rows] float32 as given, or None; read by every call, so it may be filled in place."""
+        return self._bias
 
     @classmethod
     def from_weights(cls, weight, bias=None, *, group: int = 64):

@@ -265,3 +265,17 @@ def test_sizes_beyond_32_bits_are_refused(recorder, monkeypatch):
         with pytest.raises(cb.CBInferError, match=message):
             call()
     assert not launches and not recorder.calls
+
+
+def test_tensors_that_a_layer_points_to_stay_its_own(recorder):
+    """A layer's calls read its bias, its decays and its state where they lay when it was made: they cannot be put aside while it lives."""
+    layer = cb.QuantisedLinear(torch.zeros(4, 96, dtype=torch.uint8), torch.zeros(4, 2, dtype=torch.bfloat16), torch.ones(4))
+    att = cb.LinearAttention([0.9, 0.8], 8, 8)
+    for owner, name in ((layer, "bias"), (att, "decay"), (att, "state")):
+        with pytest.raises(AttributeError):
+            setattr(owner, name, None)
+    layer(torch.zeros(1, 96))
+    att.process(*(torch.zeros(1, 1, 2, 8) for _ in range(3)))
+    product, attention = recorder.calls
+    assert product.bias == layer.bias.data_ptr()
+    assert (attention.decay, attention.state) == (att.decay.data_ptr(), att.state.data_ptr())
