@@ -14,7 +14,7 @@
  *   - Calls are asynchronous, allocate nothing and keep nothing: what they need beyond inputs and
  *     outputs is the workspace that the caller passes (256-byte aligned, of the size that the function beside
  *     the call returns, its contents of no matter before and after).  Two calls that may run at the same time need two.
- *   - Strides are in elements.  Outputs must not overlap inputs except where a call says so.
+ *   - Strides are in elements.  Outputs must not overlap themselves, nor inputs except where a call says so.
  *   - Sums, softmax statistics, states and norms are float32 at least whatever the type of the
  *     tensors; values are rounded to bfloat16 once, when they are stored.
  */

@@ -120,6 +120,16 @@ def _float32(t, device, size: int, what: str):
     _same_device(t, device, what)
 
 
+def _apart(t) -> bool:
+    """Whether no two values of a tensor to be written share their memory, as far as its axes in the order of their strides tell."""
+    reach = 0
+    for stride, size in sorted((s, n) for n, s in zip(t.shape, t.stride()) if n > 1):
+        if stride <= reach:
+            return False
+        reach += stride * (size - 1)
+    return True
+
+
 def _stream(device) -> int:
     """torch.cuda.current_stream(device).cuda_stream without the objects in between, which cost more than a launch."""
     return torch._C._cuda_getCurrentRawStream(device.index)
@@ -308,10 +318,11 @@ class LinearAttention:
         """The next tokens of every stream: q [n_streams][tokens][heads][key_size], k [..][kv_heads][key_size],
         v [..][kv_heads][value_size], the last axis contiguous; lengths: None, or int32 [n_streams], how many of the
         tokens a stream has.  Returns [n_streams][tokens][heads][value_size] and leaves the new state."""
-        geometry = (q.shape, q.stride(), k.shape, k.stride(), v.shape, v.stride(), q.dtype, k.dtype, v.dtype, lengths is None)
+        geometry = (q.shape, q.stride(), k.shape, k.stride(), v.shape, v.stride(), q.dtype, k.dtype, v.dtype, lengths is None,
+                    None if out is None else (out.shape, out.stride(), out.dtype))
         plan = self._plan
         if plan is None or plan.geometry != geometry:
-            plan = self._plan = self._planned(geometry, q, k, v, lengths)
+            plan = self._plan = self._planned(geometry, q, k, v, lengths, out)
         a = linear_attention_args.from_buffer_copy(plan.args)
         device = _device(q, "q")
         _same_device(k, device, "k")
@@ -320,9 +331,7 @@ class LinearAttention:
         if out is None:
             out = torch.empty(plan.shape, dtype=q.dtype, device=device)
         else:
-            if out.shape != plan.shape or out.dtype != q.dtype or out.device != device or (self.value_size > 1 and out.stride(3) != 1):
-                _refuse("out must be a tensor like q of shape %s" % (plan.shape,))
-            a.o_stride[:] = out.stride()[:3]
+            _same_device(out, device, "out")
         if lengths is not None:
             if lengths.dtype != torch.int32 or lengths.shape != (self.n_streams,) or not lengths.is_contiguous():
                 _refuse("lengths must be a contiguous int32 tensor of n_streams values")
@@ -335,7 +344,7 @@ class LinearAttention:
             _raise(rc)
         return out
 
-    def _planned(self, geometry, q, k, v, lengths) -> _LayerPlan:
+    def _planned(self, geometry, q, k, v, lengths, out) -> _LayerPlan:
         """Checks of shapes and types, and what follows from them; kept for calls of the same geometry."""
         a = linear_attention_args.from_buffer_copy(self._args)
         if q.dim() != 4:
@@ -354,10 +363,15 @@ class LinearAttention:
         a.dtype = _dtype(q, "q")
         a.tokens = tokens
         a.q_stride[:], a.k_stride[:], a.v_stride[:] = q.stride()[:3], k.stride()[:3], v.stride()[:3]
-        a.o_stride[:] = (tokens * self.heads * self.value_size, self.heads * self.value_size, self.value_size)
+        shape = (self.n_streams, tokens, self.heads, self.value_size)
+        if out is None:
+            a.o_stride[:] = (tokens * self.heads * self.value_size, self.heads * self.value_size, self.value_size)
+        else:
+            if out.shape != shape or out.dtype != q.dtype or (self.value_size > 1 and out.stride(3) != 1) or not _apart(out):
+                _refuse("out must be a tensor like q of shape %s, its values apart in memory" % (shape,))
+            a.o_stride[:] = out.stride()[:3]
         a.lengths = None if lengths is None else a.state  # of the workspace it matters only whether there are any
-        return _LayerPlan(geometry, a, (self.n_streams, tokens, self.heads, self.value_size),
-                          self.lib.cbinfer_linear_attention_workspace_bytes(a))
+        return _LayerPlan(geometry, a, shape, self.lib.cbinfer_linear_attention_workspace_bytes(a))
 
 
 # ---- products with 4-bit weights ------------------------------------------------------------------
@@ -566,6 +580,8 @@ def _norm_plan(x, weight, group, gate, activation, residual, next_weight, eps, s
         if sum_out.dtype != sum_kind:
             _refuse("sum_out must have the type of the residual (without one: of x)")
         _, a.h_stride = _norm_rows(sum_out, shape, "sum_out")
+        if not _apart(sum_out):
+            _refuse("sum_out: its values must lie apart in memory")
     else:
         a.h_stride = a.size
     a.y_stride = a.size

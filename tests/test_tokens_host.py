@@ -279,3 +279,24 @@ def test_tensors_that_a_layer_points_to_stay_its_own(recorder):
     product, attention = recorder.calls
     assert product.bias == layer.bias.data_ptr()
     assert (attention.decay, attention.state) == (att.decay.data_ptr(), att.state.data_ptr())
+
+
+def test_outputs_that_overlap_themselves_are_refused(recorder, monkeypatch):
+    launches = []
+    monkeypatch.setattr(tokens, "_lib", type("Lib", (), {"cbinfer_gated_norm": lambda self, a, stream: launches.append(a) or 0})())
+    att = cb.LinearAttention([0.9, 0.8], 8, 8, n_streams=2)
+    q, x = torch.zeros(2, 3, 2, 8), torch.zeros(4, 8)
+    memory = torch.zeros(500)
+    for out in (memory[:48].view(1, 3, 2, 8).expand(2, 3, 2, 8), memory.as_strided((2, 3, 2, 8), (48, 16, 7, 1)), memory.as_strided((2, 3, 2, 8), (40, 16, 8, 1))):
+        with pytest.raises(cb.CBInferError, match="out"):
+            att.process(q, q, q, out=out)
+    for out in (memory[:8].expand(4, 8), memory.as_strided((4, 8), (7, 1))):
+        with pytest.raises(cb.CBInferError, match="sum_out"):
+            cb.gated_norm(x, sum_out=out)
+    assert not launches and not recorder.calls
+    for out in (memory.as_strided((2, 3, 2, 8), (16, 32, 8, 1)), memory.as_strided((2, 3, 2, 8), (100, 30, 12, 1))):  # apart, in any order
+        assert att.process(q, q, q, out=out) is out
+        assert list(recorder.calls[-1].o_stride) == list(out.stride()[:3]) and recorder.calls[-1].o == out.data_ptr()
+    assert att.process(q, q, q) is not out and list(recorder.calls[-1].o_stride) == [48, 16, 8]
+    out = memory.as_strided((4, 8), (9, 1))
+    assert cb.gated_norm(x, sum_out=out)[0] is out and launches[0].h_stride == 9
