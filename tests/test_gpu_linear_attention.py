@@ -189,3 +189,71 @@ def test_scores_and_states_keep_24_bits(T, d, wide):
     out = att.process(*(t.bfloat16().cuda() for t in (q, k, v)))
     assert torch.equal(att.state.cpu().double(), S)
     assert torch.equal(out.cpu(), want.to(torch.bfloat16))
+
+
+def _some_heads(out, state, q, k, v, start, decay, scale, lengths, dtype, what, until=None):
+    """A sample of a larger call's streams and heads against 64 bits; until: outputs alone, of the tokens in front."""
+    B, T, H, dk = q.shape
+    share = H // k.shape[2]
+    for b, h in ((0, 0), (B - 1, H - 1), (B // 2, 1), (1, H // 2)):
+        s, g = slice(b, b + 1), slice(h, h + 1)
+        kv = slice(h // share, h // share + 1)
+        n = None if lengths is None else [lengths[b]]
+        ref = attention64(q[s, :until, g], k[s, :until, kv], v[s, :until, kv], start[s, g], decay[g], scale, n)
+        if until is None:
+            check_attention(out[s, :, g], state[s, g], ref, T, dk, dtype, "%s, stream %d, head %d" % (what, b, h))
+        else:
+            check_attention(out[s, :until, g], ref[1], ref, T, dk, dtype, "%s, stream %d, head %d" % (what, b, h))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dk,dv", [(64, 96), (64, 100), (128, 128), (128, 100), (40, 128)])
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("aligned", [True, False])
+def test_enough_heads_to_fill_the_chip(aligned, ragged, dk, dv, dtype):
+    """Streams and heads enough for workgroups of 128 columns."""
+    B, T, H, K = 8, 300, 8, 4
+    g = torch.Generator().manual_seed(dk + dv)
+    r = lambda n, d: torch.randn(B, T, n, d + 3, generator=g).to(dtype).cuda()  # noqa: E731
+    q, k, v = (t[..., :-3].contiguous() if aligned else t[..., 1:-2] for t in (r(H, dk), r(K, dk), r(K, dv)))
+    decay = [1.0 - 2.0 ** -(1.0 + h) for h in range(H)]
+    start = torch.randn(B, H, dk, dv, generator=g)
+    lengths = [300, 0, 1, 64, 65, 299, 128, 257] if ragged else None
+    n = None if lengths is None else torch.tensor(lengths, dtype=torch.int32).cuda()
+    att = cb.LinearAttention(decay, dk, dv, n_streams=B, kv_heads=K, scale=0.3)
+    att.state.copy_(start)
+    out = att.process(q, k, v, n)
+    _some_heads(out, att.state, q, k, v, start, decay, 0.3, lengths, dtype, "filled")
+    if ragged:
+        for b, length in enumerate(lengths):
+            assert not out[b, length:].any()
+        assert torch.equal(att.state[1].cpu(), start[1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dk,dv", [(64, 96), (128, 128), (128, 100)])
+def test_not_finite_among_heads_that_fill_the_chip(dk, dv, dtype):
+    """A later token that is not finite, in every stream: the outputs in front of it, in its own 64 tokens too, are as they were."""
+    B, T, H, at = 8, 300, 8, 290
+    g = torch.Generator().manual_seed(3)
+    q, k, v = (torch.randn(B, T, H, d, generator=g).to(dtype).cuda() for d in (dk, dk, dv))
+    v[:, at, :, 5], v[:, at, :, dv - 1] = float("nan"), float("inf")
+    decay = [0.9] * H
+    att = cb.LinearAttention(decay, dk, dv, n_streams=B, scale=0.3)
+    out = att.process(q, k, v)
+    _some_heads(out, None, q, k, v, torch.zeros(B, H, dk, dv), decay, 0.3, None, dtype, "in front", until=at)
+    assert not out[:, at:, :, 5].isfinite().any() and not out[:, at:, :, dv - 1].isfinite().any()
+    rest = [c for c in range(dv) if c not in (5, dv - 1)]
+    assert out[..., rest].isfinite().all() and att.state[..., rest].isfinite().all()
+
+
+@pytest.mark.parametrize("wide", ["scores", "state"])
+def test_24_bits_with_heads_that_fill_the_chip(wide):
+    T, d = 300, 128
+    q, k, v, state = _integers(T, d, 11, wide)
+    att = cb.LinearAttention([1.0] * 8, d, d, n_streams=8)
+    att.state.copy_(state)
+    want, S, _, _ = attention64(q, k, v, state, [1.0], 1.0, None)
+    out = att.process(*(t.bfloat16().cuda().expand(8, T, 8, d).contiguous() for t in (q, k, v)))
+    assert bool((att.state.cpu().double() == S).all())
+    assert bool((out.cpu() == want.to(torch.bfloat16)).all())

@@ -247,3 +247,20 @@ def test_quantising_as_many_weights_as_there_may_be(rows, cols):
     codes, scales = cb.quantise_weights(w, 32)
     for at in places:
         assert torch.equal(codes[at:at + 512], want[0]) and torch.equal(scales[at:at + 512], want[1]), at
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,k", [(300, 1500), (500, 300), (70, 20000)])
+@pytest.mark.parametrize("few,many", [(1, 16), (18, 32)])
+def test_a_token_alone_and_among_others(few, many, n, k, dtype):
+    """For 1 .. 16 tokens, and for 17 .. 32, a token's result has the same bits whatever tokens are beside it, and however many."""
+    layer = _layer(n, k, 32, 9)[3]
+    g = torch.Generator().manual_seed(5)
+    x = torch.randn(many, k, generator=g).to(dtype).cuda()
+    y = layer(x)
+    assert torch.equal(layer(x[:few]), y[:few])
+    z = x.clone()
+    z[few:] = torch.randn(many - few, k, generator=g).to(dtype).cuda()
+    z[few, 0], z[many - 1, k - 1] = float("nan"), float("inf")
+    got = layer(z)
+    assert torch.equal(got[:few], y[:few]) and got[few].isnan().all() and not got[many - 1].isfinite().any()

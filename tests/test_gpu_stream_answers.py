@@ -75,3 +75,26 @@ def test_example_runs():
     for places, answer in answers:
         assert places.top.shape == (2, 2, 12, 16) and answer.index.shape == (2, 1, 5)
         assert bool((answer.top <= 0).all()) and bool((places.entropy >= 0).all())
+
+
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+def test_frame_by_frame_and_a_short_clip(kind):
+    """Up to 16 tokens a call the block's products give a token the same bits alone and in a clip, so queries, keys and values are the same,
+    and the states differ by the roundings of their sums alone."""
+    ex = _example()
+    heads, size, B, T = 4, 64, 3, 5
+    w = ex.make_weights(500, heads, size, 200, seed=5)
+    x = torch.randn(B, T, 500, generator=torch.Generator().manual_seed(4)).to(kind).cuda()
+    head = ex.RecurrentHead(w, B, heads, size)
+    seen, process = [], head.attention.process
+    head.attention.process = lambda q, k, v: (seen.append((q, k, v)), process(q, k, v))[1]
+    head(x)
+    after = head.attention.state.clone()
+    head.reset()
+    for t in range(T):
+        head(x[:, t:t + 1])
+        for a, b in zip(seen[0], seen[-1]):
+            assert torch.equal(a[:, t:t + 1], b)
+    _, S, _, M = attention64(*seen[0], torch.zeros(B, heads, size, size), w["decay"], size ** -0.5, None)
+    for state in (after, head.attention.state):
+        assert bool(((state.cpu().double() - S).abs() <= (T + size + 32) * 2.0 ** -24 * M).all())
