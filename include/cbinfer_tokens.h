@@ -89,7 +89,9 @@ int cbinfer_linear_attention(const cbinfer_linear_attention_args *a, void *strea
  * w[n][k] = scale[n][k / group] * value(code[n][k]), value of the codes 0 .. 7: 0, 0.5, 1, 1.5, 2, 3, 4, 6, of
  * 8 .. 15 the same negative (sign, two bits of exponent, one of mantissa: the 4-bit float that this GPU converts in
  * hardware).  A group is 32, 64 or 128 weights along a row, the last of a row may be shorter.  scales are bfloat16.
- *   y[m][n] = bias[n] + sum_k x[m][k] w[n][k] */
+ *   y[m][n] = bias[n] + sum_k x[m][k] w[n][k]
+ * A group's products are added up in float32 before its scale is applied: where they pass 3.4e38 the result is not finite
+ * even if the scaled sum would be. */
 
 /* weights [rows][cols] float32 or bfloat16, finite, -> codes [rows][cols], one byte each, and scales
  * [rows][ceil(cols / group)]: the scale is a sixth of the largest magnitude of the group, rounded to bfloat16, and

@@ -128,10 +128,10 @@ hipError_t recurrent_any(hipStream_t st, const cbinfer_linear_attention_args &a)
 // have.  The two exchange half of their parts of Q S through LDS and then have 32 queries each.  Q, K, V and
 // the scores lie in LDS, the next chunk's are on their way in registers.
 //
-// A workgroup of eight waves takes 5 us for 64 tokens and a state of 128 x 128 in bfloat16: 1.4 us of matrix instructions, 2 of other
+// A workgroup of eight waves takes 6.4 us for 64 tokens and a state of 128 x 128 in bfloat16: 1.7 us of matrix instructions, 2.5 of other
 // vector instructions (splitting values most of all), three barriers, and the two waves of a SIMD hardly overlap the two kinds.
-// 8192 tokens of 16 such heads: outputs 51 us for 134 MB, the joining of 16 parts among them (without it 46; 28 with no arithmetic, 39 with
-// no loads and stores), before that what the parts leave 22, which its loads take too.
+// 8192 tokens of 16 such heads: outputs 57 us for 134 MB, the joining of 16 parts among them (without it 51), before that what the parts
+// leave 22.
 //
 // bfloat16: what is computed on the way (scores, states, faded values) enters a product as a sum of three bfloat16, 24 bits: exactly.
 // float32: the float32 instruction.

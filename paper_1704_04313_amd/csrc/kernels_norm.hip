@@ -25,7 +25,8 @@ __device__ __forceinline__ float block_sum(float v, float *scratch)
 
 // exp(-|g|), which never overflows, so that gates far below zero keep their bits down to the smallest number.  As the square of
 // 2^(-|g| log2(e) / 2), which is a normal number wherever the square is any; log2(e) / 2 in two parts, the first of which times a bfloat16
-// is exact, and what its product with a float32 is rounded by, make up for an exponent that would be off by up to 2^-18.
+// is exact, and what its product with a float32 is rounded by, make up for an exponent that would be off by up to 2^-18.  A gate is off
+// by 2^-21 of itself at most.
 template <int DT>
 __device__ __forceinline__ float exp_down(float g)
 {
@@ -47,7 +48,7 @@ __device__ __forceinline__ float gate_of(float g, int kind)
 }
 
 // Groups of any size: the row lies in LDS as float32.  One value a thread and load: 8192 rows of 4095 bfloat16 with a gate and groups of
-// 45 158 us, where rows of 4096 in groups of 64 take 42 in the kernel below.
+// 45 155 us, where rows of 4096 in groups of 64 take 43 in the kernel below.
 template <int DT, int DS>
 __global__ __launch_bounds__(256) void norm_row_kernel(const cbinfer_gated_norm_args a, int64_t first)
 {
@@ -275,9 +276,10 @@ hipError_t by_eights(hipStream_t st, const cbinfer_gated_norm_args &a)
 {
     const int eights = (int)((a.size + 7) / 8);
     const size_t lds = a.weight && a.group && a.group != a.size ? (size_t)eights * sizeof(float) : 0;
-    // A workgroup reads the weights once for all its rows: few of them pay, if they still cover the memory's latency.  us for 8192
-    // rows of 4096 with a float32 residual and both norms (470 MB) at 256, 512, 768, 1024, 8192 workgroups: 124, 96, 106, 111, 214;
-    // 8192 of 2048 with groups of 128 and a gate alone (101 MB): 42, 26, 23, 22, 34.
+    // A workgroup reads the weights once for all its rows: few of them pay, if they still cover the memory's latency.  us with 1024, 2048, 4096
+    // and 8192 waves.  Gate, float32 residual and both norms: 8192 rows of 4096 bfloat16 126, 97, 111, 117, float32 147, 132, 141, 152; 8192 of 768
+    // 36, 23, 24, 29; 3000 of 8192 86, 87, 88, 102.  A gate alone: 8192 of 4096 in groups of 64 81, 53, 43, 44; 8192 of 2048 in groups of 128 44, 27,
+    // 23, 25, float32 58, 36, 37, 40; 3000 of 8192 40, 40, 34, 37.
     const int waves = a.y ? 2048 : 4096;
     // 8192 rows of 768 bfloat16, a residual and both norms: two waves a row 23 us, four 34
     const int threads = eights <= 64 ? 256 : ((eights <= 256 ? eights : (eights + 1) / 2) + 63) / 64 * 64, rows = eights <= 64 ? 4 : 1;

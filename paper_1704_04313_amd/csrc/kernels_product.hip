@@ -74,7 +74,7 @@ __global__ __launch_bounds__(256) void pack_scales_kernel(const uint16_t *scales
     to[u] = n < rows && k < groups ? scales[n * groups + k] : (uint16_t)0;
 }
 
-// 32 lanes a group; 100003 x 2048 float32 436 us.
+// 32 lanes a group; 100003 x 2048 float32 447 us, not bound by memory (bfloat16, half the bytes: 484).
 template <int DT>
 __global__ __launch_bounds__(256) void quantise_kernel(const typename Elem<DT>::type *w, int64_t rows, int64_t cols, int64_t stride, int group, int64_t groups, int64_t first, uint8_t *codes, uint16_t *scales)
 {
@@ -367,7 +367,7 @@ auto with_shape(const cbinfer_quantised_product_args &a, F f)
         if (a.tokens > 32 && tiles >= 1024) {
             // three tiles of tokens at a time, 48 tokens, 100003 x 2048: 47, four 58; 37 tokens, 56488 x 1310: 29, 35
             if (a.tokens <= 48) return f(Shape<DT, 3, 2, 2, 8, 1>());
-            // 64 tokens, 100003 x 2048 in groups of 128: 16 waves 62, eight with two blocks each 73; 20000 x 1500: 18.1, 20.5
+            // 64 tokens, 100003 x 2048 in groups of 128: 16 waves 56, eight with two blocks each 72; 20000 x 1500: 17.2, 20.7
             if (blocks <= 16) return f(Shape<DT, 4, 1, 1, 16, 1>());
             // 256 tokens, 20000 x 4096: 97, 16 waves 105, two tiles of tokens 115
             return f(Shape<DT, 4, 2, 2, 8, 1>());

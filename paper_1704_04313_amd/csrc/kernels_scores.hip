@@ -253,8 +253,8 @@ __device__ void finish(const cbinfer_log_probs_args &a, int64_t pos, int64_t bas
     }
 }
 
-// One wave a position, any strides, one class a lane at a time: bound by how many lines of memory its loads touch (2048 rows of 4000
-// bfloat16 classes, two apart: 42 us).
+// One wave a position, any strides, one class a lane at a time, one load of a wave under way: bound by their latency.  2048 rows of 4000
+// bfloat16 classes, two apart (33 MB of lines): 7.6 us for the sums, 12.6 with 5 alternatives.
 template <int DT>
 __global__ __launch_bounds__(256) void wave_kernel(const cbinfer_log_probs_args a, int64_t first, FastDiv inner)
 {
@@ -624,8 +624,8 @@ __device__ void careful_top_lane(const cbinfer_log_probs_args &a, int64_t base, 
 
 // PARTS > 1: the waves of a workgroup share the classes of 256 / PARTS positions, for maps that would not fill the chip
 // otherwise.  CH classes are loaded while those before are worked on.  Bound by memory without alternatives or with few (64 x 8 x 180 x
-// 320 float32, 3 alternatives: 221 MB in 39 us), by the network's instructions with more (10 x 256 x 180 x 320, 590 MB of float32: 109 us
-// without, 127 with 8; bfloat16 67 and 110).  Where a class lies is the same for every lane, where a position lies does not change: an
+// 320 float32, 3 alternatives: 221 MB in 40 us), by the network's instructions with more (10 x 256 x 180 x 320, 590 MB of float32: 110 us
+// without, 127 with 8; bfloat16 64 and 100).  Where a class lies is the same for every lane, where a position lies does not change: an
 // address costs no vector instruction (with 64 bits a lane and a bounds check for each: 119, 143, 80 and 132).
 template <int DT, int K, int PARTS>
 __global__ __launch_bounds__(256) void map_kernel(const cbinfer_log_probs_args a, FastDiv inner)
@@ -755,7 +755,8 @@ Plan plan(const cbinfer_log_probs_args &a)
     const int64_t positions = a.outer * a.inner;
     if (a.class_stride == 1) {
         p.kind = kRows;
-        // us a call, 4096 rows of 1000 bfloat16: a wave each 17, four waves each 32
+        // us a call with 5 alternatives, a wave each and four waves each.  4096 rows bfloat16: 1000 classes 12.6, 20.7, 2048 17.1, 20.1, 4000 24.6,
+        // 19.9; float32 11.7, 22.6, 18.2, 22.4, 26.7, 22.9.  512 rows of 2048 bfloat16 11.1, 10.8, of 4000 16.4, 11.4.
         if (a.classes <= 2048) return p;
         p.waves = 4;
         // Few long rows are cut into segments of one or two rounds of loads, up to 1024 workgroups, and joined by a second launch.
@@ -764,8 +765,11 @@ Plan plan(const cbinfer_log_probs_args &a)
         if (segments >= 4) p.segments = (int)segments;
     } else if (a.classes <= 1 << 30 && a.inner_stride == 1 && a.inner >= 16 && (a.outer == 1 || a.outer_stride >= a.inner) && a.top <= 16 && (a.classes <= 1024 || positions >= 16384) &&
                (a.dtype == kF32 || a.classes <= Key<kBF16>::kClasses)) {
+        // A lane a position or a wave each, us with 3 alternatives: 2000 maps of 64 classes and 16 positions 10.8, 46, of 8 (taken by waves) 10.6, 26;
+        // float32 the same.  Many classes need as many positions: 4 x 2000 classes x 256 positions bfloat16 38, 25, 4 x 2000 x 1024 39, 39, 16 x 2000 x
+        // 1024 39, 130; 4 x 1024 x 256 20, 16, 4 x 1024 x 1024 21, 23.
         p.kind = kMaps; // counts classes in whole rounds and parts, in 32 bits
-        // 5 x 191 x 148 x 269 bfloat16, 3 alternatives: a wave each 35 us, four waves 29; float32 without: 28, 33
+        // 5 x 191 x 148 x 269 bfloat16, 3 alternatives: a wave each 34 us, four waves 29; float32 without: 29.5, 34
         p.waves = positions < (a.top ? 262144 : 65536) && a.classes >= 32 ? 4 : 1;
     }
     return p;
